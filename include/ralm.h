@@ -317,6 +317,167 @@ ralm_status_t ralm_merge_lists(const int64_t *ids, const float *scores, const in
 ralm_status_t ralm_debug_fail_allocation(int32_t nth);
 ralm_status_t ralm_selftest_wait_timeout(int64_t limit_cycles, int32_t *device_status, void *stream);
 
+/* ---- The generator's side of the serving loop -------------------------------------------------
+ * What a server does with the retrieved neighbours, the drafted tokens and its key-value cache next
+ * to retrieval and verification: the KNN-LM mixture (Section 5.3: softmax over the negative distances
+ * of the neighbours, interpolated with the model's distribution), verification of drafted tokens
+ * against the target's probabilities, the pages of a cache (roll back = give pages back, asynchronous
+ * verification = fork), and a cache held in 4 bits with the attention that reads it. All pointers are
+ * DEVICE pointers unless stated; every call is asynchronous on `stream` and allocates nothing. */
+
+typedef enum { RALM_F16 = 0, RALM_BF16 = 1, RALM_F32 = 2 } ralm_dtype_t;
+
+#define RALM_MAX_VOCAB (1 << 22) /* entries of a row of logits or probabilities */
+
+/* The KNN-LM mixture, for R rows:
+ *   probs[v] = (1 - lambda) softmax(logits / temperature)[v] + lambda sum over {i: values[ids[i]] = v} w[i]
+ *   w = softmax(-scores / knn_temperature) for RALM_L2, softmax(+scores / knn_temperature) for RALM_IP.
+ *   logits  [R][V] in `dtype`, row pitch ld_logits elements; -inf marks a token that cannot come.
+ *   ids, scores  [R][k] as ralm_search wrote them, 0 <= k <= RALM_MAX_K. An id outside [0, N), a value
+ *           outside [0, V) and a score that is not finite are left out (padding of a short list).
+ *   values  int32 [N], the token that follows each datastore entry.
+ *   probs   fp32 [R][V], row pitch ld_probs (written).
+ * A row with no neighbour left is softmax(logits / temperature) alone (k == 0 asks for just that), a
+ * row whose logits are all -inf is the neighbours' distribution alone, a row with neither is zeros. A
+ * NaN or +inf among the logits makes the row NaN, as in a softmax. Neighbours' weights are added in
+ * fixed point: the result does not depend on the order of the atomics.
+ * Errors: INVALID_ARG (null pointers, sizes, pitch < V, lambda outside [0, 1], temperatures not
+ * positive and finite, dtype or metric unknown). R == 0 is a no-op. */
+ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_logits, int32_t R, int32_t V,
+                           const int64_t *ids, const float *scores, int32_t k, ralm_metric_t metric,
+                           const int32_t *values, int64_t N, float lambda, float temperature,
+                           float knn_temperature, float *probs, int64_t ld_probs, void *stream);
+
+/* Verification of drafted tokens from given random numbers, for R requests of up to S drafts:
+ * position i is accepted while uniforms[i] * draft_probs[i][t_i] < target_probs[i][t_i] (fp32 product);
+ * at the first rejection `a` a token is drawn from max(target_probs[a] - draft_probs[a], 0), after a
+ * full acceptance from target_probs[n], n the number of drafts.
+ *   draft_tokens  int64 [R][S]; a token outside [0, V) is rejected.
+ *   draft_probs   fp32 [R][S][V] with pitches draft_ld_r and draft_ld_s, or NULL: the drafts came
+ *                 with certainty (draft_probs = 1 at the token and 0 elsewhere).
+ *   target_probs  fp32 [R][S + 1][V] with pitches target_ld_r and target_ld_s.
+ *   uniforms      fp32 [R][S + 1] in [0, 1); the last one draws the token.
+ *   draft_len     int32 [R], drafts of each request (clamped to 0..S), or NULL: S.
+ *   tokens        int64 [R][S + 1] (written): the accepted drafts, the drawn token, then -1.
+ *   accepted      int32 [R] (written): accepted drafts; the M that ralm_os3_gamma takes.
+ * The draw: with w[v] = floor(2^40 x[v]), x clamped to [0, 1] and NaN as 0, T = sum w and
+ * t = floor(T * floor(2^24 u) / 2^24), it is the first v with w[0] + .. + w[v] > t. Whole numbers: the
+ * token does not depend on how the row is split. If nothing is left of the difference the draw is
+ * from target_probs[a]; if that row is empty too the token is -1.
+ * Errors: INVALID_ARG. R == 0 is a no-op. */
+ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft_probs, int64_t draft_ld_r,
+                                 int64_t draft_ld_s, const float *target_probs, int64_t target_ld_r,
+                                 int64_t target_ld_s, const float *uniforms, const int32_t *draft_len, int32_t R,
+                                 int32_t S, int32_t V, int64_t *tokens, int32_t *accepted, void *stream);
+
+/* A paged cache. The struct lives in host memory, what it points to on the device.
+ *   pool         layers x pages x page_bytes bytes, layers layer_stride bytes apart (may be NULL where
+ *                only the bookkeeping is wanted); 16-byte aligned, page_bytes and layer_stride multiples
+ *                of 16.
+ *   table        [rows][max_pages]: the pages of each row, in order; -1 where there is none.
+ *   lengths      [rows]: tokens of each row; a row holds ceil(length / page_size) pages.
+ *   refs         [pages]: holders of each page; 0 is free.
+ *   status       [1]: sticky status word, see ralm_pages_status.
+ *   workspace    ralm_pages_workspace(pages) bytes, ZEROED by the caller before the first call.
+ * One pool may be used from one stream at a time. A caller starts from zeroed lengths and refs and a
+ * table of -1. */
+typedef struct {
+    void *pool;
+    int64_t layers, layer_stride, page_bytes;
+    int32_t pages, rows, max_pages, page_size;
+    int32_t *table, *lengths, *refs, *status;
+    void *workspace;
+} ralm_pages_t;
+
+#define RALM_MAX_ROWS 65536          /* rows of a page table */
+#define RALM_MAX_ROW_PAGES (1 << 20) /* pages of one row */
+
+/* Bytes of the workspace of a pool of so many pages (host arithmetic). */
+int64_t ralm_pages_workspace(int32_t pages);
+
+/* Set every row's length: shorter rows give pages back (0 frees the row: roll back, evict), longer
+ * rows take the lowest-numbered free pages in row order (after all rows have given back). A longer row
+ * whose last page is not full and is held by other rows too gets a copy of it first, in every layer
+ * (copy on write); if all holders of such a page grow in one call, the lowest row keeps it.
+ * new_lengths int32 [rows]. If the free pages do not suffice (status word RALM_ERR_OOM), or a length
+ * is outside 0 .. max_pages * page_size (RALM_ERR_INVALID_ARG), the call changes nothing. */
+ralm_status_t ralm_pages_resize(const ralm_pages_t *pages, const int32_t *new_lengths, void *stream);
+
+/* Fork: row dst[i] gives back what it holds and then holds the pages and the length of row src[i],
+ * i < n, without copying. A destination may not occur twice nor also be a source; such a call, or one
+ * with a row outside the table, changes nothing (status word RALM_ERR_INVALID_ARG). */
+ralm_status_t ralm_pages_fork(const ralm_pages_t *pages, const int32_t *src, const int32_t *dst, int32_t n,
+                              void *stream);
+
+/* Compact: the live pages become pages 0 .. live - 1. The i-th live page at or above `live` moves to the
+ * i-th hole below it, with its contents in every layer; the table follows. live: int32 [1] (written). */
+ralm_status_t ralm_pages_compact(const ralm_pages_t *pages, int32_t *live, void *stream);
+
+/* Copy the contents of src->pool pages from[i] to dst->pool pages to[i], i < n, in every layer (copying
+ * out of and into a pool; tables and holders stay as they are). page_bytes and layers must agree. A
+ * pair outside the pools is left out (dst's status word RALM_ERR_INVALID_ARG). No page may be written
+ * twice, nor read and written, in one call. */
+ralm_status_t ralm_pages_copy(const ralm_pages_t *src, const int32_t *from, const ralm_pages_t *dst,
+                              const int32_t *to, int32_t n, void *stream);
+
+/* Read and clear the status word (synchronises the stream): RALM_OK, RALM_ERR_OOM,
+ * RALM_ERR_INVALID_ARG. The larger one stays if several came. */
+ralm_status_t ralm_pages_status(const ralm_pages_t *pages, void *stream);
+
+/* A key-value cache held in 4 bits over such a pool: page_bytes = kv_heads * page_size * (head_dim + 8),
+ * head_dim 64 or 128, page_size 16, 32 or 64. A vector of one token and head is held as
+ *   s = fp16((max - min) / 15), b = fp16(min + 8 s), c = clamp(rint((x - b) / s) + 8, 0, 15)
+ * and stands for s (c - 8) + b. Values saturate at +-57344; a NaN counts as 0. */
+typedef struct {
+    ralm_pages_t pages;
+    int32_t kv_heads, head_dim;
+} ralm_kv_t;
+
+/* K and V of n tokens for each of `batch` entries: [batch][n][kv_heads][head_dim] in RALM_F16 or
+ * RALM_BF16, the last dimension contiguous, strides in elements. */
+typedef struct {
+    void *k, *v;
+    int64_t k_stride_b, k_stride_n, k_stride_h, v_stride_b, v_stride_n, v_stride_h;
+    int32_t batch, n;
+    ralm_dtype_t dtype;
+    const int32_t *rows;   /* [batch] row of the table of each entry, or NULL: entry i is row i */
+    const int32_t *starts; /* [batch] position of each entry's first token */
+    const int32_t *count;  /* [batch] tokens of each entry (at most n), or NULL: n */
+} ralm_kv_tokens_t;
+
+/* Quantise the tokens into positions starts .. starts + count - 1, which lie below the row's length
+ * (ralm_pages_resize first) in pages that no other row holds. Others are left out, and the status word
+ * says RALM_ERR_INVALID_ARG. */
+ralm_status_t ralm_kv_append(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream);
+
+/* The values that positions starts .. starts + n - 1 stand for; zeros at positions outside the row or
+ * beyond `count`. */
+ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream);
+
+/* Attention of the newest tokens over the cache: query i of an entry with m = q_len queries (n where
+ * q_len is NULL) stands at position length - m + i and sees the keys up to and including it. One token per
+ * entry is a decode step, drafts + 1 of them a verification. Queries that see nothing, and those at
+ * or beyond q_len, give zeros.
+ *   q, out   [batch][n][q_heads][head_dim], fp16 or bf16, strides in elements, last dimension contiguous;
+ *            q_heads a multiple of kv_heads, query head h reads key-value head h / (q_heads / kv_heads).
+ *   workspace of ralm_kv_attend_workspace(...) bytes, 16-byte aligned; needs no initial value. */
+typedef struct {
+    const void *q;
+    void *out;
+    int64_t q_stride_b, q_stride_n, q_stride_h, out_stride_b, out_stride_n, out_stride_h;
+    int32_t batch, n, q_heads;
+    ralm_dtype_t dtype;
+    float scale;
+    const int32_t *rows, *q_len; /* [batch] each, may be NULL */
+    void *workspace;
+    int64_t workspace_bytes;
+} ralm_attend_t;
+
+#define RALM_MAX_ATTEND_BATCH 4096
+
+int64_t ralm_kv_attend_workspace(int32_t kv_heads, int32_t head_dim, int32_t q_heads, int32_t n);
+ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_attend_t *attend, void *stream);
+
 /* Static description of a status code. */
 const char *ralm_status_string(ralm_status_t status);
 

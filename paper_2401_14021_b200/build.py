@@ -12,7 +12,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libralm.so")
 DEBUG_LIB = os.path.join(HERE, "libralm_debug.so")
-SOURCES = ["ralm_api.cu", "os3.cpp"]
+SOURCES = ["ralm_api.cu", "generate_api.cu", "os3.cpp"]
 HEADERS = ["common.cuh", "scan.cuh", "aux_kernels.cuh", os.path.join("..", "..", "include", "ralm.h")]
 
 

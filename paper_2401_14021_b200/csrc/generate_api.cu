@@ -1,0 +1,397 @@
+// Host side of the generator's operators declared in include/ralm.h: the KNN-LM mixture, verification
+// of drafted tokens, the pages of a cache, and the 4-bit cache with its attention. Argument checks and
+// launches only; nothing here allocates.
+#include "../../include/ralm.h"
+
+#include <cuda_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <cmath>
+
+#include "attend.cuh"
+#include "kv4.cuh"
+#include "mix.cuh"
+#include "pages.cuh"
+#include "verify_tokens.cuh"
+
+using namespace ralm;
+
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// SMs of the current device (0: none), asked once per device.
+int sm_count() {
+    static std::atomic<int> known[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return 0;
+    int n = dev < 64 ? known[dev].load(std::memory_order_relaxed) : 0;
+    if (n == 0) {
+        if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+        if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+ralm_status_t launched() { return cudaGetLastError() == cudaSuccess ? RALM_OK : RALM_ERR_CUDA; }
+
+// Lets a kernel use up to `most` bytes of dynamic shared memory; asked once per kernel and device.
+template <auto Kernel>
+bool allow_smem(int most) {
+    static std::atomic<bool> done[64];
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0) return false;
+    if (dev < 64 && done[dev].load(std::memory_order_relaxed)) return true;
+    if (cudaFuncSetAttribute(Kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most) != cudaSuccess) {
+        cudaGetLastError();
+        return false;
+    }
+    if (dev < 64) done[dev].store(true, std::memory_order_relaxed);
+    return true;
+}
+
+// One cluster of `cluster` CTAs per row.
+template <typename Params>
+ralm_status_t launch_cluster(void (*kernel)(Params), int rows, int cluster, int threads, size_t smem, cudaStream_t st,
+                             const Params &params) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(rows) * cluster);
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = cluster;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, params) != cudaSuccess) {
+        cudaGetLastError();
+        return RALM_ERR_CUDA;
+    }
+    return RALM_OK;
+}
+
+constexpr int kMixMaxStage = 160 * 1024;   // bytes of a row slice that a CTA keeps in shared memory
+
+template <typename T>
+ralm_status_t launch_mix(MixParams p, int R, int sms, cudaStream_t st) {
+    constexpr int64_t kVec = MixVec<T>::n;
+    int cluster = 1;
+    auto slice_of = [&](int c) { return ((p.V + kVec - 1 + c - 1) / c + kVec - 1) / kVec * kVec; };
+    while (cluster < kMixMaxCluster && (static_cast<int64_t>(R) * cluster < 4LL * sms || slice_of(cluster) * sizeof(T) > 64 * 1024) &&
+           slice_of(2 * cluster) >= 2 * kMixThreads)
+        cluster *= 2;
+    p.slice = static_cast<int>(slice_of(cluster));
+    const size_t bytes = p.slice * sizeof(T);
+    if (bytes <= kMixMaxStage && !allow_smem<mix_kernel<T, true>>(kMixMaxStage)) return RALM_ERR_CUDA;
+    if (bytes <= kMixMaxStage) return launch_cluster(mix_kernel<T, true>, R, cluster, kMixThreads, bytes, st, p);
+    return launch_cluster(mix_kernel<T, false>, R, cluster, kMixThreads, 0, st, p);
+}
+
+bool pages_ok(const ralm_pages_t *p) {
+    return p && p->pages >= 0 && p->rows >= 0 && p->rows <= RALM_MAX_ROWS && p->max_pages >= 1 &&
+           p->max_pages <= RALM_MAX_ROW_PAGES && p->page_size >= 1 &&
+           static_cast<int64_t>(p->max_pages) * p->page_size < (int64_t{1} << 31) - 1 &&
+           (p->rows == 0 || (p->table && p->lengths)) && (p->pages == 0 || p->refs) && p->status && p->workspace;
+}
+bool pool_ok(const ralm_pages_t *p) {
+    return p->pool && aligned16(p->pool) && p->layers >= 1 && p->layers <= (1 << 20) && p->page_bytes >= 16 && p->page_bytes % 16 == 0 &&
+           p->layer_stride % 16 == 0 && (p->layers == 1 || p->layer_stride >= p->page_bytes * p->pages);
+}
+ralm_status_t launch_copy(const PagesCopyParams &p, int64_t most, cudaStream_t st) {
+    const int sms = sm_count();
+    if (sms == 0) return RALM_ERR_CUDA;
+    const int64_t jobs = most * std::max(p.layers, 1) * ((p.page_bytes + 16383) / 16384);
+    const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(jobs, 8LL * sms));
+    pages_copy_kernel<<<static_cast<int>(blocks), kCopyThreads, 0, st>>>(p);
+    return launched();
+}
+PagesCopyParams copy_in_pool(const ralm_pages_t &p) {
+    PagesCopyParams c = {};
+    c.src = c.dst = static_cast<unsigned char *>(p.pool);
+    c.src_layer_stride = c.dst_layer_stride = p.layer_stride;
+    c.page_bytes = p.page_bytes;
+    c.layers = p.pool ? static_cast<int>(p.layers) : 0;
+    c.src_pages = c.dst_pages = p.pages;
+    const PagesWork w = pages_work(p);
+    c.from = w.from;
+    c.to = w.to;
+    c.count = w.head;
+    return c;
+}
+
+bool kv_ok(const ralm_kv_t *c, int32_t layer) {
+    if (!c || !pages_ok(&c->pages) || !pool_ok(&c->pages)) return false;
+    const ralm_pages_t &p = c->pages;
+    return c->kv_heads >= 1 && c->kv_heads <= 4096 && (p.page_size == 16 || p.page_size == 32 || p.page_size == 64) && layer >= 0 &&
+           layer < p.layers && p.page_bytes == static_cast<int64_t>(c->kv_heads) * p.page_size * (c->head_dim + 8);
+}
+KvParams kv_params(const ralm_kv_t &c, int32_t layer, const int32_t *rows, int batch) {
+    const ralm_pages_t &p = c.pages;
+    KvParams k;
+    k.layer = static_cast<unsigned char *>(p.pool) + layer * p.layer_stride;
+    k.page_bytes = p.page_bytes;
+    k.table = p.table;
+    k.lengths = p.lengths;
+    k.refs = p.refs;
+    k.status = p.status;
+    k.table_rows = p.rows;
+    k.max_pages = p.max_pages;
+    k.pages = p.pages;
+    k.page_size = p.page_size;
+    k.heads = c.kv_heads;
+    k.rows = rows;
+    k.batch = batch;
+    return k;
+}
+
+template <typename T, int D>
+ralm_status_t launch_tokens(bool append, const KvParams &k, const KvTokens &t, int sms, cudaStream_t st) {
+    const int64_t jobs = static_cast<int64_t>(k.batch) * t.n * k.heads;
+    const int blocks = static_cast<int>(std::min<int64_t>((jobs + kKvThreads / 32 - 1) / (kKvThreads / 32), 32LL * sms));
+    if (append) kv_append_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
+    else kv_read_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
+    return launched();
+}
+ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ralm_kv_tokens_t *t, void *stream) {
+    if (!kv_ok(c, layer) || !t || t->batch < 0 || t->n < 0 || (t->dtype != RALM_F16 && t->dtype != RALM_BF16))
+        return RALM_ERR_INVALID_ARG;
+    if (c->head_dim != 64 && c->head_dim != 128) return RALM_ERR_UNSUPPORTED;
+    if (t->batch == 0 || t->n == 0) return RALM_OK;
+    if (!t->k || !t->v || !t->starts) return RALM_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return RALM_ERR_CUDA;
+    const KvParams k = kv_params(*c, layer, t->rows, t->batch);
+    const KvTokens x = {t->k, t->v, t->k_stride_b, t->k_stride_n, t->k_stride_h, t->v_stride_b, t->v_stride_n, t->v_stride_h,
+                        t->n, t->starts, t->count};
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (t->dtype == RALM_F16)
+        return c->head_dim == 64 ? launch_tokens<__half, 64>(append, k, x, sms, st) : launch_tokens<__half, 128>(append, k, x, sms, st);
+    return c->head_dim == 64 ? launch_tokens<__nv_bfloat16, 64>(append, k, x, sms, st)
+                             : launch_tokens<__nv_bfloat16, 128>(append, k, x, sms, st);
+}
+
+// Column blocks of 8 query rows that one pass over the keys serves.
+int attend_nt(int rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
+int attend_workers(int nt, int sms) { return sms * (nt <= 2 ? 2 : 1) * kAttendWarps; }
+
+template <typename T, int D, int NT>
+ralm_status_t launch_attend(AttendParams p, int sms, cudaStream_t st) {
+    const size_t smem = (p.kv.batch + 1) * sizeof(int);
+    p.workers = attend_workers(NT, sms);
+    p.part = p.part_ml + static_cast<int64_t>(2) * p.workers * 8 * NT * 2;
+    attend_kernel<T, D, NT><<<p.workers / kAttendWarps, kAttendThreads, smem, st>>>(p);
+    ralm_status_t rs = launched();
+    if (rs != RALM_OK) return rs;
+    const dim3 grid(static_cast<unsigned>(p.kv.batch) * p.kv.heads * p.row_blocks, std::min(8 * NT, p.n * p.group));
+    attend_join_kernel<T, D, 8 * NT><<<grid, D, smem, st>>>(p);
+    return launched();
+}
+template <typename T, int D>
+ralm_status_t launch_attend(const AttendParams &p, int nt, int sms, cudaStream_t st) {
+    if (nt == 1) return launch_attend<T, D, 1>(p, sms, st);
+    if (nt == 2) return launch_attend<T, D, 2>(p, sms, st);
+    return launch_attend<T, D, 4>(p, sms, st);
+}
+
+}  // namespace
+
+extern "C" {
+
+ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_logits, int32_t R, int32_t V,
+                           const int64_t *ids, const float *scores, int32_t k, ralm_metric_t metric,
+                           const int32_t *values, int64_t N, float lambda, float temperature,
+                           float knn_temperature, float *probs, int64_t ld_probs, void *stream) {
+    if (R < 0 || V < 1 || V > RALM_MAX_VOCAB || ld_logits < V || ld_probs < V || k < 0 || k > RALM_MAX_K || N < 0)
+        return RALM_ERR_INVALID_ARG;
+    if (dtype != RALM_F16 && dtype != RALM_BF16 && dtype != RALM_F32) return RALM_ERR_INVALID_ARG;
+    if (metric != RALM_IP && metric != RALM_L2) return RALM_ERR_INVALID_ARG;
+    if (!(lambda >= 0.f && lambda <= 1.f) || !(temperature > 0.f) || !(knn_temperature > 0.f) || std::isinf(temperature) ||
+        std::isinf(knn_temperature))
+        return RALM_ERR_INVALID_ARG;
+    if (R == 0) return RALM_OK;
+    if (!logits || !probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
+    if (reinterpret_cast<uintptr_t>(logits) % (dtype == RALM_F32 ? 4 : 2) != 0) return RALM_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(R) * kMixMaxCluster >= (int64_t{1} << 31)) return RALM_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return RALM_ERR_CUDA;
+    MixParams p;
+    p.logits = logits;
+    p.ld_logits = ld_logits;
+    p.V = V;
+    p.ids = ids;
+    p.scores = scores;
+    p.k = k;
+    p.values = values;
+    p.N = N;
+    p.score_scale = (metric == RALM_L2 ? -kLog2e : kLog2e) / knn_temperature;
+    p.logit_scale = kLog2e / temperature;
+    p.lambda = lambda;
+    p.probs = probs;
+    p.ld_probs = ld_probs;
+    p.slice = 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (dtype == RALM_F16) return launch_mix<__half>(p, R, sms, st);
+    if (dtype == RALM_BF16) return launch_mix<__nv_bfloat16>(p, R, sms, st);
+    return launch_mix<float>(p, R, sms, st);
+}
+
+ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft_probs, int64_t draft_ld_r,
+                                 int64_t draft_ld_s, const float *target_probs, int64_t target_ld_r,
+                                 int64_t target_ld_s, const float *uniforms, const int32_t *draft_len, int32_t R,
+                                 int32_t S, int32_t V, int64_t *tokens, int32_t *accepted, void *stream) {
+    if (R < 0 || S < 0 || S > (1 << 20) || V < 1 || V > RALM_MAX_VOCAB) return RALM_ERR_INVALID_ARG;
+    if (R == 0) return RALM_OK;
+    if ((S > 0 && !draft_tokens) || !target_probs || !uniforms || !tokens || !accepted) return RALM_ERR_INVALID_ARG;
+    if (static_cast<int64_t>(R) * kVtMaxCluster >= (int64_t{1} << 31)) return RALM_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return RALM_ERR_CUDA;
+    VerifyTokensParams p;
+    p.draft = draft_tokens;
+    p.draft_probs = S > 0 ? draft_probs : nullptr;
+    p.draft_ld_r = draft_ld_r;
+    p.draft_ld_s = draft_ld_s;
+    p.target_probs = target_probs;
+    p.target_ld_r = target_ld_r;
+    p.target_ld_s = target_ld_s;
+    p.uniforms = uniforms;
+    p.draft_len = draft_len;
+    p.S = S;
+    p.V = V;
+    p.tokens = tokens;
+    p.accepted = accepted;
+    int cluster = 1;
+    while (cluster < kVtMaxCluster && static_cast<int64_t>(R) * cluster < 4LL * sms && V / (2 * cluster) >= 2 * kVtThreads) cluster *= 2;
+    p.slice = (V + cluster - 1) / cluster;
+    return launch_cluster(verify_tokens_kernel, R, cluster, kVtThreads, 0, static_cast<cudaStream_t>(stream), p);
+}
+
+int64_t ralm_pages_workspace(int32_t pages) {
+    return pages < 0 ? 0 : pages_workspace_words(pages) * static_cast<int64_t>(sizeof(int32_t));
+}
+
+ralm_status_t ralm_pages_resize(const ralm_pages_t *pages, const int32_t *new_lengths, void *stream) {
+    if (!pages_ok(pages) || (pages->pool && !pool_ok(pages))) return RALM_ERR_INVALID_ARG;
+    if (pages->rows == 0) return RALM_OK;
+    if (!new_lengths) return RALM_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    pages_resize_kernel<<<1, kPagesThreads, 0, st>>>(*pages, new_lengths);
+    ralm_status_t rs = launched();
+    if (rs != RALM_OK || !pages->pool) return rs;
+    return launch_copy(copy_in_pool(*pages), std::min(pages->rows, pages->pages), st);   // at most one page per row
+}
+
+ralm_status_t ralm_pages_fork(const ralm_pages_t *pages, const int32_t *src, const int32_t *dst, int32_t n, void *stream) {
+    if (!pages_ok(pages) || n < 0 || n > pages->rows) return RALM_ERR_INVALID_ARG;
+    if (n == 0) return RALM_OK;
+    if (!src || !dst) return RALM_ERR_INVALID_ARG;
+    pages_fork_kernel<<<1, kPagesThreads, (pages->rows + 31) / 32 * sizeof(int), static_cast<cudaStream_t>(stream)>>>(*pages, src, dst, n);
+    return launched();
+}
+
+ralm_status_t ralm_pages_compact(const ralm_pages_t *pages, int32_t *live, void *stream) {
+    if (!pages_ok(pages) || (pages->pool && !pool_ok(pages)) || !live) return RALM_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    pages_compact_kernel<<<1, kPagesThreads, 0, st>>>(*pages, live);
+    ralm_status_t rs = launched();
+    if (rs != RALM_OK) return rs;
+    PagesCopyParams c = copy_in_pool(*pages);
+    c.table = pages->table;
+    c.table_words = static_cast<int64_t>(pages->rows) * pages->max_pages;
+    c.remap = pages_work(*pages).list;
+    c.remap_pages = pages->pages;
+    return launch_copy(c, std::max<int64_t>(pages->pages / 2, c.table_words / (kCopyThreads * 8)), st);
+}
+
+ralm_status_t ralm_pages_copy(const ralm_pages_t *src, const int32_t *from, const ralm_pages_t *dst, const int32_t *to,
+                              int32_t n, void *stream) {
+    if (!src || !dst || n < 0 || !pool_ok(src) || !pool_ok(dst) || src->page_bytes != dst->page_bytes || src->layers != dst->layers)
+        return RALM_ERR_INVALID_ARG;
+    if (n == 0) return RALM_OK;
+    if (!from || !to || !dst->status) return RALM_ERR_INVALID_ARG;
+    PagesCopyParams c = {};
+    c.src = static_cast<const unsigned char *>(src->pool);
+    c.dst = static_cast<unsigned char *>(dst->pool);
+    c.src_layer_stride = src->layer_stride;
+    c.dst_layer_stride = dst->layer_stride;
+    c.page_bytes = src->page_bytes;
+    c.layers = static_cast<int>(src->layers);
+    c.src_pages = src->pages;
+    c.dst_pages = dst->pages;
+    c.from = from;
+    c.to = to;
+    c.n = n;
+    c.status = dst->status;
+    return launch_copy(c, n, static_cast<cudaStream_t>(stream));
+}
+
+ralm_status_t ralm_pages_status(const ralm_pages_t *pages, void *stream) {
+    if (!pages || !pages->status) return RALM_ERR_INVALID_ARG;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    int word = 0;
+    if (cudaMemcpyAsync(&word, pages->status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
+        cudaMemsetAsync(pages->status, 0, sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
+        return RALM_ERR_CUDA;
+    if (word == kStatusNoPages) return RALM_ERR_OOM;
+    if (word == kStatusInvalid) return RALM_ERR_INVALID_ARG;
+    return word == 0 ? RALM_OK : RALM_ERR_CUDA;
+}
+
+ralm_status_t ralm_kv_append(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream) {
+    return kv_tokens(true, cache, layer, tokens, stream);
+}
+ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream) {
+    return kv_tokens(false, cache, layer, tokens, stream);
+}
+
+int64_t ralm_kv_attend_workspace(int32_t kv_heads, int32_t head_dim, int32_t q_heads, int32_t n) {
+    if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads != 0 || n < 0 || (head_dim != 64 && head_dim != 128)) return 0;
+    const int64_t rows = static_cast<int64_t>(q_heads / kv_heads) * n;
+    const int nt = attend_nt(static_cast<int>(std::min<int64_t>(rows, 1 << 20)));
+    return static_cast<int64_t>(2) * attend_workers(nt, std::max(sm_count(), 1)) * 8 * nt * (head_dim + 2) * sizeof(float);
+}
+
+ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_attend_t *a, void *stream) {
+    if (!kv_ok(cache, layer) || !a || a->batch < 0 || a->batch > RALM_MAX_ATTEND_BATCH || a->n < 0 || a->q_heads < 1 ||
+        a->q_heads % cache->kv_heads != 0 || (a->dtype != RALM_F16 && a->dtype != RALM_BF16) || !std::isfinite(a->scale))
+        return RALM_ERR_INVALID_ARG;
+    if (cache->head_dim != 64 && cache->head_dim != 128) return RALM_ERR_UNSUPPORTED;
+    if (a->batch == 0 || a->n == 0) return RALM_OK;
+    if (!a->q || !a->out || !a->workspace || !aligned16(a->workspace)) return RALM_ERR_INVALID_ARG;
+    const int group = a->q_heads / cache->kv_heads;
+    const int64_t rows = static_cast<int64_t>(group) * a->n;
+    const ralm_pages_t &pg = cache->pages;
+    if (rows > (1 << 20) ||
+        static_cast<int64_t>(a->batch) * ((static_cast<int64_t>(pg.max_pages) * pg.page_size + 15) / 16) >= (int64_t{1} << 31))
+        return RALM_ERR_UNSUPPORTED;
+    if (a->workspace_bytes < ralm_kv_attend_workspace(cache->kv_heads, cache->head_dim, a->q_heads, a->n)) return RALM_ERR_INVALID_ARG;
+    const int sms = sm_count();
+    if (sms == 0) return RALM_ERR_CUDA;
+    const int nt = attend_nt(static_cast<int>(rows));
+    AttendParams p;
+    p.kv = kv_params(*cache, layer, a->rows, a->batch);
+    p.q = a->q;
+    p.out = a->out;
+    p.q_b = a->q_stride_b;
+    p.q_n = a->q_stride_n;
+    p.q_h = a->q_stride_h;
+    p.o_b = a->out_stride_b;
+    p.o_n = a->out_stride_n;
+    p.o_h = a->out_stride_h;
+    p.q_len = a->q_len;
+    p.n = a->n;
+    p.group = group;
+    p.row_blocks = static_cast<int>((rows + 8 * nt - 1) / (8 * nt));
+    p.scale = a->scale * kLog2e;
+    p.part_ml = static_cast<float *>(a->workspace);
+    p.vec = aligned16(a->q) && a->q_stride_b % 8 == 0 && a->q_stride_n % 8 == 0 && a->q_stride_h % 8 == 0;
+    if (static_cast<int64_t>(a->batch) * cache->kv_heads * p.row_blocks >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (a->dtype == RALM_F16)
+        return cache->head_dim == 64 ? launch_attend<__half, 64>(p, nt, sms, st) : launch_attend<__half, 128>(p, nt, sms, st);
+    return cache->head_dim == 64 ? launch_attend<__nv_bfloat16, 64>(p, nt, sms, st) : launch_attend<__nv_bfloat16, 128>(p, nt, sms, st);
+}
+
+}  // extern "C"

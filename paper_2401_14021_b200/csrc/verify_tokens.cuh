@@ -1,0 +1,168 @@
+// Verification of drafted tokens against the target's probabilities from given random numbers
+// (speculative sampling): position i is accepted while u_i q_i[t_i] < p_i[t_i]; at the first
+// rejection the token is drawn from max(p - q, 0), after a full acceptance from the next row of p.
+//
+// The draw inverts a cumulative sum whose terms are whole numbers, w = floor(2^40 x): integer sums
+// have no order, so any split over lanes, warps and CTAs gives the same token.
+#pragma once
+
+#include <cooperative_groups.h>
+#include <stdint.h>
+
+#include "common.cuh"
+
+namespace ralm {
+
+constexpr int kVtThreads = 512;
+constexpr int kVtWarps = kVtThreads / 32;
+constexpr int kVtMaxCluster = 8;
+
+struct VerifyTokensParams {
+    const int64_t *draft;        // [R][S]
+    const float *draft_probs;    // or null: the draft was certain of its tokens
+    int64_t draft_ld_r, draft_ld_s;
+    const float *target_probs;
+    int64_t target_ld_r, target_ld_s;
+    const float *uniforms;       // [R][S + 1]
+    const int32_t *draft_len;    // or null
+    int S, V, slice;             // slice: elements of a row that one CTA handles
+    int64_t *tokens;             // [R][S + 1]
+    int32_t *accepted;           // [R]
+};
+
+// floor(2^40 min(max(x, 0), 1)), NaN counts as 0
+__device__ __forceinline__ uint64_t fixed40(float x) {
+    x = fminf(fmaxf(x, 0.f), 1.f);
+    const uint32_t bits = __float_as_uint(x);
+    const uint64_t m = static_cast<uint64_t>((bits & 0x7FFFFFu) | 0x800000u) << 17;   // x = m 2^(e - 127 - 40)
+    const int down = 127 - static_cast<int>(bits >> 23);
+    return down < 41 ? m >> down : 0;
+}
+__device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+
+// One cluster per request. CTA c sums the weights of elements [c * slice, (c + 1) * slice), each warp
+// a run of its own; the sums say which run holds the drawn token, and that CTA looks for it there.
+__global__ void __launch_bounds__(kVtThreads)
+verify_tokens_kernel(const VerifyTokensParams p) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    const int C = cluster.num_blocks(), c = cluster.block_rank();
+    const int r = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    __shared__ uint64_t peers[2][kVtMaxCluster];
+    __shared__ uint64_t warp_total[kVtWarps];
+    __shared__ int first;
+    const int64_t *draft = p.draft + static_cast<int64_t>(r) * p.S;
+    const float *u = p.uniforms + static_cast<int64_t>(r) * (p.S + 1);
+    const float *target = p.target_probs + r * p.target_ld_r;
+    const float *dprobs = p.draft_probs ? p.draft_probs + r * p.draft_ld_r : nullptr;
+    const int n = p.draft_len ? min(max(p.draft_len[r], 0), p.S) : p.S;
+
+    if (warp == 0) {
+        int a = n;
+        for (int i0 = 0; i0 < n; i0 += 32) {
+            const int i = i0 + lane;
+            bool ok = true;
+            if (i < n) {
+                const int64_t t = draft[i];
+                ok = false;
+                if (t >= 0 && t < p.V) {
+                    const float q = dprobs ? dprobs[i * p.draft_ld_s + t] : 1.f;
+                    ok = __fmul_rn(u[i], q) < target[i * p.target_ld_s + t];
+                }
+            }
+            const uint32_t bad = __ballot_sync(0xffffffffu, !ok);
+            if (bad) {
+                a = i0 + __ffs(bad) - 1;
+                break;
+            }
+        }
+        if (lane == 0) first = a;
+    }
+    __syncthreads();
+    const int a = first;
+    const float *prow = target + a * p.target_ld_s;
+    const float *qrow = a < n && dprobs ? dprobs + a * p.draft_ld_s : nullptr;
+    const int64_t gone = a < n && !dprobs ? draft[a] : -1;   // a certain draft: its token leaves the row
+
+    const int lo = min(c * p.slice, p.V), hi = min(lo + p.slice, p.V);
+    const int run = ((hi - lo + kVtWarps - 1) / kVtWarps + 31) & ~31;
+    auto weight = [&](int v, bool whole) -> uint64_t {
+        float x = prow[v];
+        if (!whole) {
+            if (qrow) x = __fsub_rn(x, qrow[v]);
+            if (v == gone) x = 0.f;
+        }
+        return fixed40(x);
+    };
+    int64_t *out = p.tokens + static_cast<int64_t>(r) * (p.S + 1);
+    if (c == 0) {
+        for (int i = tid; i <= p.S; i += kVtThreads)
+            if (i != a) out[i] = i < a ? draft[i] : -1;
+        if (tid == 0) p.accepted[r] = a;
+    }
+    // the residual; should nothing be left of it, the target's row itself
+    for (int round = 0; round < 2; ++round) {
+        const bool whole = round == 1 || a >= n;
+        const int w0 = min(lo + warp * run, hi), w1 = min(w0 + run, hi);
+        uint64_t sum = 0;
+#pragma unroll 8
+        for (int v = w0 + lane; v < w1; v += 32) sum += weight(v, whole);
+        sum = warp_sum_u64(sum);
+        if (lane == 0) warp_total[warp] = sum;
+        if (round == 0) cluster.sync(); else __syncthreads();   // warp totals; every CTA of the cluster runs
+        uint64_t total = 0;
+        for (int i = 0; i < kVtWarps; ++i) total += warp_total[i];
+        if (tid < C) *cluster.map_shared_rank(&peers[round][c], tid) = total;
+        cluster.sync();
+        uint64_t T = 0, before = 0;
+        for (int i = 0; i < C; ++i) {
+            if (i < c) before += peers[round][i];
+            T += peers[round][i];
+        }
+        if (T == 0) {                                           // the same for the whole cluster
+            if (!whole) continue;
+            if (c == 0 && tid == 0) out[a] = -1;                // no token has any probability
+            break;
+        }
+        const float us = u[p.S];
+        const uint64_t U = min(static_cast<uint32_t>(fminf(fmaxf(us, 0.f), 1.f) * 16777216.f), 16777215u);
+        const uint64_t t = U * (T >> 32) * 256 + (U * (T & 0xFFFFFFFFull) >> 24);
+        if (t < before || t >= before + total) break;      // another CTA of the cluster has it
+        // the run that holds it, then the element: each thread a few consecutive ones
+        uint64_t at = before;
+        int w = 0;
+        while (w < kVtWarps - 1 && t >= at + warp_total[w]) at += warp_total[w++];
+        const int r0 = min(lo + w * run, hi), r1 = min(r0 + run, hi);
+        const int each = (r1 - r0 + kVtThreads - 1) / kVtThreads;
+        const int e0 = min(r0 + tid * each, r1), e1 = min(e0 + each, r1);
+        uint64_t mine = 0;
+        for (int v = e0; v < e1; ++v) mine += weight(v, whole);
+        uint64_t scan = mine;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const uint64_t y = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += y;
+        }
+        __syncthreads();
+        if (lane == 31) warp_total[warp] = scan;
+        __syncthreads();
+        for (int i = 0; i < warp; ++i) at += warp_total[i];
+        at += scan - mine;
+        if (t >= at && t < at + mine) {
+            int v = e0;
+            for (;; ++v) {
+                const uint64_t x = weight(v, whole);
+                if (t < at + x || v == e1 - 1) break;
+                at += x;
+            }
+            out[a] = v;
+        }
+        break;
+    }
+}
+
+}  // namespace ralm
