@@ -1,10 +1,19 @@
 // Attention of a request's newest tokens over its 4-bit cache:
 //     out = softmax(scale q.k) v over the keys that the query may see.
 //
-// With k = s_k (c - 8) + b_k the score is s_k (q.(c - 8)) + b_k sum(q), and the output is
-// sum (p s_v)(c - 8) + sum p b_v: the matrix instructions see whole numbers between -8 and 7, exact in
-// fp16, and the scales enter in 32 bits. The weights p s_v are rounded to fp16 (11 bits) before the
-// second product; maxima, sums and outputs stay in 32 bits.
+// With k = s_k (c - 8) + b_k the score is s_k q.c + (b_k - 8 s_k) sum(q), and the output is
+// sum (p s_v)(c - 8) + sum p b_v: the matrix instructions see whole numbers, and the scales enter in 32 bits.
+// A code needs no conversion: four bits in the lowest places of an fp16 word ARE the number c 2^-24, and in
+// the next four c 2^-20, subnormals that the instructions take exactly. One masking instruction makes an
+// operand of two codes; the powers of two go into q and the results. The 8 matters in the second product
+// only, where thousands of weights would pile up 7.5 times their sum beside a small difference: it is taken
+// from the operand (one instruction, shared by all query rows), or with a single block of 8 query rows by a
+// second product of the weights with a constant -8, which the matrix pipe has time for.
+// The weights p s_v are rounded to fp16 (11 bits) before the second product; maxima, sums and outputs stay in
+// 32 bits.
+//
+// A warp is a worker with its own stages in shared memory (bulk copies of 32 tokens, completion on a
+// barrier of its own): no warp waits for another, and any mix of lengths keeps all of them busy.
 //
 // Orientation: keys are the rows of the instructions (m16n8k16) and query rows the columns, so that a
 // decode step with up to 8 query rows per key-value head fills one column block, and the codes go from
@@ -23,12 +32,27 @@
 
 namespace ralm {
 
-constexpr int kAttendThreads = 256;
-constexpr int kAttendWarps = kAttendThreads / 32;
 constexpr int kAttendMaxBatch = 4096;
-constexpr int kAttendMinTiles = 4;       // a worker is given at least this many tiles of 16 tokens
+constexpr int kAttendStage = 64;         // tokens of a stage in shared memory, the largest unit of work
 constexpr float kAttendLazy = 6.f;       // a maximum may be this far (powers of two) behind before sums are rescaled
 constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8 + 1) is below fp16's largest
+constexpr int kJoinThreads = 256;
+
+// Warps per CTA (one CTA per SM) and whether the query operands stay in registers, by column blocks.
+__host__ __device__ constexpr int attend_warps(int nt, int d) { return nt >= 3 ? 8 : nt == 1 && d == 64 ? 16 : 12; }
+__host__ __device__ constexpr bool attend_q_in_regs(int nt) { return nt == 1; }
+// Shared memory of a warp: stages of kAttendStage tokens and, where they are not in registers, the queries.
+__host__ __device__ constexpr int attend_stage_bytes(int d) { return kAttendStage * (d + 8); }
+__host__ __device__ constexpr int attend_q_bytes(int nt, int d) { return attend_q_in_regs(nt) ? 0 : 16 * nt * d; }
+constexpr int kAttendSmem = 207 * 1024;  // for the warps; the prefix sums and static variables take the rest
+__host__ __device__ constexpr int attend_stages(int nt, int d) {
+    const int fit = (kAttendSmem / attend_warps(nt, d) - attend_q_bytes(nt, d)) / attend_stage_bytes(d);
+    return fit > 4 ? 4 : fit;
+}
+__host__ __device__ constexpr int attend_warp_bytes(int nt, int d) {
+    return attend_stages(nt, d) * attend_stage_bytes(d) + attend_q_bytes(nt, d);
+}
+static_assert(attend_stages(1, 128) >= 2 && attend_stages(2, 128) >= 1 && attend_stages(4, 128) >= 2, "stages");
 
 struct AttendParams {
     KvParams kv;
@@ -42,32 +66,39 @@ struct AttendParams {
     float *part;              // [2 * workers][8 * NT][D] partial outputs
     float *part_ml;           // [2 * workers][8 * NT][2] their maxima and sums
     int workers;
+    int page_shift;           // log2 of the page size
     int vec;                  // q is 16-byte aligned in every row
 };
 
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t x) {
     uint32_t y;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
 __device__ __forceinline__ uint32_t hsub2(uint32_t a, uint32_t b) {
     const __half2 r = __hsub2(*reinterpret_cast<__half2 *>(&a), *reinterpret_cast<__half2 *>(&b));
     return *reinterpret_cast<const uint32_t *>(&r);
 }
-// The four pairs (nibble i of the low half, nibble i of the high half) of a word as fp16 pairs minus 8:
-// a nibble under the exponent of 1024 (in the last four mantissa bits) or of 64 (in the four above)
-// reads 1024 + c or 64 + c, and the subtraction is exact.
+// The four pairs (nibble i of the low half, nibble i of the high half) of a word as fp16 numbers: c 2^-24
+// for i = 0 and 2, c 2^-20 for i = 1 and 3.
 __device__ __forceinline__ void unpack4(uint32_t x, uint32_t (&y)[4]) {
     const uint32_t z = x >> 8;
-    y[0] = hsub2((x & 0x000F000Fu) | 0x64006400u, 0x64086408u);   // - 1032
-    y[1] = hsub2((x & 0x00F000F0u) | 0x54005400u, 0x54805480u);   // - 72
-    y[2] = hsub2((z & 0x000F000Fu) | 0x64006400u, 0x64086408u);
-    y[3] = hsub2((z & 0x00F000F0u) | 0x54005400u, 0x54805480u);
+    y[0] = x & 0x000F000Fu;
+    y[1] = x & 0x00F000F0u;
+    y[2] = z & 0x000F000Fu;
+    y[3] = z & 0x00F000F0u;
+}
+
+// The same as c - 8: exact, the difference of two multiples of 2^-24.
+__device__ __forceinline__ void unpack4_centred(uint32_t x, uint32_t (&y)[4]) {
+    unpack4(x, y);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = hsub2(y[i], i % 2 == 0 ? 0x00080008u : 0x00800080u);
 }
 
 template <int D> struct LaneCodes;                                    // a lane's D / 8 bytes of a tile
@@ -77,33 +108,29 @@ template <int D> __device__ __forceinline__ void load_codes(LaneCodes<D> &c, con
     c.raw = *reinterpret_cast<const decltype(c.raw) *>(at);
 }
 
-// What one tile of 16 tokens brings to a lane: codes of keys g and g + 8, V codes of its two halves, and
-// the (scale, offset) pairs of keys g and g + 8.
-template <int D> struct Tile {
-    LaneCodes<D> k[2], v[2];
-    __half2 kp[2], vp[2];
-};
-
-// How the work is cut: segments (entry, head, row block) follow one another, each `tiles` long (at least
-// one, so that an entry without keys is written too), and worker w takes units [total w / W, total (w + 1) / W).
+// How the work is cut: segments (entry, head, row block) follow one another, each `units` long (at least
+// one, so that an entry without keys is written too), and worker w, a warp, takes units
+// [total w / W, total (w + 1) / W): any mix of lengths is balanced to one unit. A unit is 64 tokens, or
+// 32 where there are so few that the warps would get less than two of them each.
 struct Share {
     long long total;
-    int workers;
+    int workers, shift;                  // log2 of a unit's tokens
     __device__ __forceinline__ long long begin(int w) const { return total * w / workers; }
     __device__ __forceinline__ int owner(long long u) const { return static_cast<int>(((u + 1) * workers - 1) / total); }
 };
-// Prefix sums of the entries' tiles (without heads and row blocks) in shared memory: cum[b] for b <= batch.
-__device__ inline Share attend_share(const AttendParams &p, int *cum, int *scratch) {
+// Inclusive prefix sums of the entries' units (without heads and row blocks) in shared memory: cum[b + 1]
+// for b < batch. Returns the whole.
+__device__ inline int attend_prefix(const AttendParams &p, int shift, int *cum, int *scratch) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int carry = 0;
     for (int b0 = 0; b0 < p.kv.batch; b0 += blockDim.x) {
         const int b = b0 + tid;
-        int tiles = 0;
+        int units = 0;
         if (b < p.kv.batch) {
             const int row = kv_row(p.kv, b);
-            tiles = row < 0 ? 1 : max((kv_length(p.kv, row) + 15) >> 4, 1);
+            units = row < 0 ? 1 : max((kv_length(p.kv, row) + (1 << shift) - 1) >> shift, 1);
         }
-        int scan = tiles;
+        int scan = units;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
             const int y = __shfl_up_sync(0xffffffffu, scan, o);
@@ -122,12 +149,57 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
     }
     if (tid == 0) cum[0] = 0;
     __syncthreads();
+    return carry;
+}
+__device__ inline Share attend_share(const AttendParams &p, int *cum, int *scratch) {
+    const long long per = static_cast<long long>(p.kv.heads) * p.row_blocks;
     Share s;
-    s.total = static_cast<long long>(carry) * p.kv.heads * p.row_blocks;
-    s.workers = static_cast<int>(min(static_cast<long long>(p.workers), max(s.total / kAttendMinTiles, 1LL)));
+    if (p.kv.batch <= (int)blockDim.x) {   // both cuts from one look at the lengths, packed in 64 bits
+        const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+        unsigned long long units = 0;
+        if (tid < p.kv.batch) {
+            const int row = kv_row(p.kv, tid);
+            const int len = row < 0 ? 0 : kv_length(p.kv, row);
+            units = static_cast<unsigned long long>(max((len + 63) >> 6, 1)) << 32 | max((len + 31) >> 5, 1);
+        }
+        unsigned long long scan = units;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const unsigned long long y = __shfl_up_sync(0xffffffffu, scan, o);
+            if (lane >= o) scan += y;
+        }
+        unsigned long long *sums = reinterpret_cast<unsigned long long *>(scratch);
+        if (lane == 31) sums[warp] = scan;
+        __syncthreads();
+        unsigned long long before = 0, all = 0;
+        const int warps = (p.kv.batch + 31) >> 5;
+        for (int i = 0; i < warps; ++i) {
+            if (i < warp) before += sums[i];
+            all += sums[i];
+        }
+        s.shift = 6;
+        s.total = static_cast<long long>(all >> 32) * per;
+        if (s.total < 2LL * p.workers) {
+            s.shift = 5;
+            s.total = static_cast<long long>(all & 0xFFFFFFFFull) * per;
+        }
+        const unsigned long long to = before + scan;
+        if (tid < p.kv.batch) cum[tid + 1] = static_cast<int>(s.shift == 6 ? to >> 32 : to);
+        if (tid == 0) cum[0] = 0;
+        __syncthreads();
+        s.workers = static_cast<int>(min(static_cast<long long>(p.workers), s.total));
+        return s;
+    }
+    s.shift = 6;
+    s.total = attend_prefix(p, 6, cum, scratch) * per;
+    if (s.total < 2LL * p.workers) {
+        s.shift = 5;
+        s.total = attend_prefix(p, 5, cum, scratch) * per;
+    }
+    s.workers = static_cast<int>(min(static_cast<long long>(p.workers), s.total));
     return s;
 }
-struct Segment { int b, h, rb, tile, tiles; };                     // tile: the unit's place inside the segment
+struct Segment { int b, h, rb, unit, units; };                     // unit: place inside the segment
 __device__ __forceinline__ Segment attend_segment(const AttendParams &p, const int *cum, long long unit) {
     const int per = p.kv.heads * p.row_blocks;
     int lo = 0, hi = p.kv.batch - 1;
@@ -137,13 +209,21 @@ __device__ __forceinline__ Segment attend_segment(const AttendParams &p, const i
     }
     Segment s;
     s.b = lo;
-    s.tiles = cum[lo + 1] - cum[lo];
+    s.units = cum[lo + 1] - cum[lo];
     const long long in = unit - static_cast<long long>(cum[lo]) * per;
-    const int which = static_cast<int>(in / s.tiles);
-    s.tile = static_cast<int>(in % s.tiles);
+    const int which = static_cast<int>(in / s.units);
+    s.unit = static_cast<int>(in - static_cast<long long>(which) * s.units);
     s.h = which / p.row_blocks;
-    s.rb = which % p.row_blocks;
+    s.rb = which - s.h * p.row_blocks;
     return s;
+}
+__device__ __forceinline__ void attend_next(const AttendParams &p, const int *cum, Segment &s) {   // the segment after s
+    s.unit = 0;
+    if (++s.rb < p.row_blocks) return;
+    s.rb = 0;
+    if (++s.h < p.kv.heads) return;
+    s.h = 0;
+    if (++s.b < p.kv.batch) s.units = cum[s.b + 1] - cum[s.b];
 }
 
 // One query row's place: query i and head of the group, from its number in the segment's entry.
@@ -154,27 +234,115 @@ __device__ __forceinline__ void attend_store(const AttendParams &p, const Segmen
     o[d] = from_float<T>(x);
 }
 
+
+// The stream of a worker's stages: which unit is asked for next. All lanes keep the same state except
+// `held`, where lane i holds table entry base + i of the row that is being read.
+struct AttendFeed {
+    Segment seg;
+    int units_left;            // of the worker
+    int len, row, slot;        // slot: the stage that is filled next
+    int held, base;
+    __device__ __forceinline__ void enter(const AttendParams &p) {
+        row = kv_row(p.kv, seg.b);
+        len = row < 0 ? 0 : kv_length(p.kv, row);
+        base = -64;
+    }
+    // Makes sure that entries index .. index + 3 are held.
+    __device__ __forceinline__ void hold(const AttendParams &p, int index, int lane) {
+        if (index >= base && index + 3 < base + 32) return;
+        base = index;
+        held = index + lane < p.kv.max_pages ? p.kv.table[static_cast<int64_t>(row) * p.kv.max_pages + index + lane] : 0;
+        if (index + lane < ((len - 1) >> p.page_shift) + 1 && (held < 0 || held >= p.kv.pages)) {
+            atomicMax(p.kv.status, kStatusInvalid);
+            held = 0;
+        }
+    }
+};
+
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(kAttendThreads, NT <= 2 ? 2 : 1)
+__global__ void __launch_bounds__(attend_warps(NT, D) * 32, 1)
 attend_kernel(const AttendParams p) {
-    constexpr int W = D / 32;            // words of K codes per lane and key; also E, dimensions / 32
+    constexpr int WARPS = attend_warps(NT, D);
+    constexpr int W = D / 32;            // words of K codes per lane and key; also dimensions / 32
     constexpr int MT = D / 16;           // row blocks of the output
     constexpr int ROWS = 8 * NT;
-    extern __shared__ int attend_smem[];
-    int *cum = attend_smem;
-    __shared__ int scratch[32];
+    constexpr int STAGES = attend_stages(NT, D);
+    constexpr int STAGE = attend_stage_bytes(D);
+    constexpr bool QREG = attend_q_in_regs(NT);
+    constexpr int KT = NT == 1 ? 2 : 1;  // tiles that are worked on side by side
+    extern __shared__ __align__(128) unsigned char attend_smem[];
+    __shared__ __align__(8) int scratch[64];
+    __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
+    unsigned char *ring = attend_smem + warp * attend_warp_bytes(NT, D);
+    uint4 *q_smem = reinterpret_cast<uint4 *>(ring + STAGES * STAGE);
+    int *cum = reinterpret_cast<int *>(attend_smem + WARPS * attend_warp_bytes(NT, D));
+    const uint32_t bar0 = smem_u32(&bars[warp * STAGES]), ring0 = smem_u32(ring);
+    if (lane == 0) {
+        for (int i = 0; i < STAGES; ++i) mbar_init(bar0 + 8 * i, 1);
+        mbar_fence_init();
+    }
     const Share share = attend_share(p, cum, scratch);
-    const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const int worker = blockIdx.x * kAttendWarps + (threadIdx.x >> 5);
+    cudaTriggerProgrammaticLaunchCompletion();
+    const int worker = blockIdx.x * WARPS + warp;
     if (worker >= share.workers) return;
-    const int ps = p.kv.page_size;
+    const int psh = p.page_shift, ps = 1 << psh;
     const int head_bytes = ps * (D + 8);
-    long long unit = share.begin(worker);
-    const long long stop = share.begin(worker + 1);
+    const int unit_tokens = 1 << share.shift;
+    const int units = static_cast<int>(share.begin(worker + 1) - share.begin(worker));
 
-    while (unit < stop) {
-        const Segment seg = attend_segment(p, cum, unit);
-        const int tiles = static_cast<int>(min(stop - unit, static_cast<long long>(seg.tiles - seg.tile)));
+    // A stage mirrors the layout of the pages that its unit lies in: page j of the unit at j * head_bytes,
+    // the parts of a page at their own offsets. Half a page is four copies, a whole one is one.
+    AttendFeed feed;
+    feed.seg = attend_segment(p, cum, share.begin(worker));
+    feed.units_left = units;
+    feed.slot = 0;
+    feed.enter(p);
+    auto issue = [&]() {                 // one unit into the next stage; its barrier completes when it has arrived
+        if (feed.units_left == 0) return;
+        const uint32_t bar = bar0 + 8 * feed.slot, dst = ring0 + feed.slot * STAGE;
+        const int tok = feed.seg.unit << share.shift;
+        if (tok < feed.len) {
+            const int index = tok >> psh;
+            feed.hold(p, index, lane);
+            const unsigned char *src = p.kv.layer + feed.seg.h * head_bytes;
+            if (unit_tokens < ps) {
+                const int page = __shfl_sync(0xffffffffu, feed.held, index - feed.base);
+                if (lane == 0) {
+                    src += page * p.kv.page_bytes;
+                    const int o = tok & (ps - 1), codes = unit_tokens * (D / 2), pairs = unit_tokens * 4;
+                    mbar_arrive_expect_tx(bar, 2 * codes + 2 * pairs);
+                    const int at[4] = {o * (D / 2), (ps + o) * (D / 2), ps * D + o * 4, ps * (D + 4) + o * 4};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) bulk_load(dst + at[i], src + at[i], i < 2 ? codes : pairs, bar);
+                }
+            } else {
+                const int count = min((unit_tokens - 1) >> psh, (feed.len - 1 - tok) >> psh) + 1;   // pages with tokens of the unit
+                if (lane == 0) mbar_arrive_expect_tx(bar, count * head_bytes);
+                for (int i = 0; i < count; ++i) {
+                    const int page = __shfl_sync(0xffffffffu, feed.held, index + i - feed.base);
+                    if (lane == 0) bulk_load(dst + i * head_bytes, src + page * p.kv.page_bytes, head_bytes, bar);
+                }
+            }
+        } else if (lane == 0) {
+            mbar_arrive(bar);            // an entry without keys
+        }
+        feed.slot = feed.slot + 1 == STAGES ? 0 : feed.slot + 1;
+        --feed.units_left;
+        if (++feed.seg.unit == feed.seg.units && feed.units_left > 0) {
+            const int b = feed.seg.b;
+            attend_next(p, cum, feed.seg);
+            if (feed.seg.b != b) feed.enter(p);
+        }
+    };
+    Segment seg = feed.seg;
+#pragma unroll 1
+    for (int i = 0; i < STAGES; ++i) issue();
+
+    int done = 0, slot = 0;
+    uint32_t parity = 0;
+    while (done < units) {
+        const int mine = min(units - done, seg.units - seg.unit);
         const int row = kv_row(p.kv, seg.b);
         const int len = row < 0 ? 0 : kv_length(p.kv, row);
         const int n = p.q_len ? min(max(p.q_len[seg.b], 0), p.n) : p.n;
@@ -182,19 +350,19 @@ attend_kernel(const AttendParams p) {
 
         // ---- the query rows: column `g` of block nt is row rb * ROWS + 8 nt + g; a lane holds dimensions
         // (D / 4) t + 8 w + q and + 4 of it for w < W, q < 4
-        uint32_t qf[NT][W][4];
+        uint32_t qf[QREG ? NT : 1][W][4];
         float qsum[NT][2];
         int last[NT][2];                 // the newest key that columns 2 t and 2 t + 1 see
         float f = 1.f;
         {
-            float top = 0.f;
+            // bring the rows to [2^10, 2^11) by one power of two: bf16 fits fp16, and 16 q does too
+            float top = 0.f, inv = 1.f;
 #pragma unroll
-            for (int pass = 0; pass < (sizeof(T) == 2 && !std::is_same<T, __half>::value ? 2 : 1); ++pass) {
-                float inv = 1.f;
-                if (pass == 1) {         // bf16: bring the rows into fp16's range by one power of two
+            for (int pass = 0; pass < 2; ++pass) {
+                if (pass == 1) {
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const int e = top > 0.f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 8, -100), 100) : 0;
+                    const int e = top > 0.f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 10, -100), 117) : 0;
                     f = __uint_as_float((127 + e) << 23);
                     inv = __uint_as_float((127 - e) << 23);
                 }
@@ -202,7 +370,7 @@ attend_kernel(const AttendParams p) {
                 for (int nt = 0; nt < NT; ++nt) {
                     const int qr = seg.rb * ROWS + nt * 8 + g;
                     const bool real = qr < rows;
-                    const int i = real ? qr / p.group : 0, gq = real ? qr % p.group : 0;
+                    const int i = real ? qr / p.group : 0, gq = real ? qr - i * p.group : 0;
                     const T *src = static_cast<const T *>(p.q) + seg.b * p.q_b + i * p.q_n +
                                    (static_cast<int64_t>(seg.h) * p.group + gq) * p.q_h + t * (D / 4);
                     float sum = 0.f;
@@ -216,17 +384,30 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                                 for (int j = 0; j < 8; ++j) u.x[j] = src[8 * w + j];
                         }
+                        if (pass == 0) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                const float x = fabsf(to_float(u.x[j]));
+                                if (x < INFINITY) top = fmaxf(top, x);
+                            }
+                            continue;
+                        }
+                        uint32_t packed[4];
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
-                            const float x0 = to_float(u.x[j]) * inv, x1 = to_float(u.x[j + 4]) * inv;
-                            if (fabsf(x0) < INFINITY) top = fmaxf(top, fabsf(x0));
-                            if (fabsf(x1) < INFINITY) top = fmaxf(top, fabsf(x1));
-                            const __half2 h = __floats2half2_rn(x0, x1);
-                            qf[nt][w][j] = *reinterpret_cast<const uint32_t *>(&h);
+                            const __half2 h = __floats2half2_rn(to_float(u.x[j]) * inv, to_float(u.x[j + 4]) * inv);
                             const float2 back = __half22float2(h);
                             sum += back.x + back.y;
+                            const __half2 up = j % 2 == 0 ? __hmul2(h, __float2half2_rn(16.f)) : h;   // c 2^-24 against c 2^-20
+                            packed[j] = *reinterpret_cast<const uint32_t *>(&up);
                         }
+                        if (QREG)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) qf[QREG ? nt : 0][w][j] = packed[j];
+                        else
+                            q_smem[(nt * W + w) * 32 + lane] = make_uint4(packed[0], packed[1], packed[2], packed[3]);
                     }
+                    if (pass == 0) continue;
                     sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                     sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
@@ -238,136 +419,202 @@ attend_kernel(const AttendParams p) {
                 }
             }
         }
-        f *= p.scale;
+        f *= p.scale * 1048576.f;        // the codes' 2^-20
 
-        float acc[NT][MT][4], m[NT][2], l[NT][2], ob[NT][2];
+        // acc is in units of 2^-24 or 2^-20 / v_unit, the weights are 2^(score - mb), mb a maximum less kAttendBias
+        float acc[NT][MT][4], mb[NT][2], l[NT][2], ob[NT][2];
+        float v_unit = 1.f, v_limit = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-            for (int e = 0; e < 2; ++e) m[nt][e] = -1e30f, l[nt][e] = ob[nt][e] = 0.f;
+            for (int e = 0; e < 2; ++e) mb[nt][e] = -1e30f, l[nt][e] = ob[nt][e] = 0.f;
 #pragma unroll
             for (int i = 0; i < MT; ++i)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) acc[nt][i][j] = 0.f;
         }
 
-        const int32_t *pages = p.kv.table + static_cast<int64_t>(max(row, 0)) * p.kv.max_pages;
-        auto fetch = [&](Tile<D> &x, int tile) {
-            const int tok = tile * 16;
-            int page = pages[tok / ps];
-            if (page < 0 || page >= p.kv.pages) {
-                atomicMax(p.kv.status, kStatusInvalid);
-                page = 0;
-            }
-            const int slot = tok % ps;
-            const unsigned char *base = p.kv.layer + page * p.kv.page_bytes + static_cast<int64_t>(seg.h) * head_bytes;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                load_codes<D>(x.k[j], base + (slot + 8 * j) * (D / 2) + lane * (D / 8));
-                load_codes<D>(x.v[j], base + ps * (D / 2) + slot * (D / 2) + j * (4 * D) + lane * (D / 8));
-                x.kp[j] = *reinterpret_cast<const __half2 *>(base + ps * D + (slot + g + 8 * j) * 4);
-                x.vp[j] = *reinterpret_cast<const __half2 *>(base + ps * (D + 4) + (slot + g + 8 * j) * 4);
-            }
-        };
-        const int first_tile = seg.tile, end_tile = len > 0 ? seg.tile + tiles : seg.tile;
-        Tile<D> next;
-        if (first_tile < end_tile) fetch(next, first_tile);
-        for (int tile = first_tile; tile < end_tile; ++tile) {
-            Tile<D> x = next;
-            if (tile + 1 < end_tile) fetch(next, tile + 1);
-            // ---- scores of keys g, g + 8 against columns 2 t, 2 t + 1
-            float sc[NT][4];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) sc[nt][j] = 0.f;
-#pragma unroll
-            for (int w = 0; w < W; ++w) {
-                uint32_t a[4], b[4];
-                unpack4(x.k[0].w[w], a);
-                unpack4(x.k[1].w[w], b);
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    mma_f16(sc[nt], a[0], b[0], a[1], b[1], qf[nt][w][0], qf[nt][w][1]);
-                    mma_f16(sc[nt], a[2], b[2], a[3], b[3], qf[nt][w][2], qf[nt][w][3]);
+        for (int u = 0; u < mine; ++u) {
+            bool here = mbar_try_wait(bar0 + 8 * slot, parity);
+            if (!here) here = mbar_wait_bounded(bar0 + 8 * slot, parity);
+            if (!__all_sync(0xffffffffu, here)) {
+                // a copy did not arrive: say so, give the others a chance to land, and leave
+                if (lane == 0) atomicMax(p.kv.status, kStatusTimeout);
+                for (int i = 1; i < STAGES && i < units - done; ++i) {
+                    slot = slot + 1 == STAGES ? 0 : slot + 1;
+                    parity ^= slot == 0;
+                    mbar_wait_bounded(bar0 + 8 * slot, parity);
                 }
+                return;
             }
-            const int key0 = tile * 16 + g;
-            float ks[2], kb[2], vs[2], vb[2], ve[2];
+            ++done;
+            const int tok0 = (seg.unit + u) << share.shift;
+            const unsigned char *st = ring + slot * STAGE;
+            // KT tiles of 16 tokens at a time; MASKED: some query does not see all of them
+            auto tile = [&](auto masked_type, int h) {
+                constexpr bool masked = decltype(masked_type)::value;
+                const int tok = tok0 + 16 * h;
+                LaneCodes<D> xk[KT][2], xv[KT][2];
+                float ks[KT][2], kb[KT][2], vs[KT][2], vb[KT][2];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const float2 a = __half22float2(x.kp[j]), b = __half22float2(x.vp[j]);
-                ks[j] = a.x * f;
-                kb[j] = a.y * f;
-                const bool inside = key0 + 8 * j < len;             // the rest of a page holds anything
-                vs[j] = inside ? b.x : 0.f;
-                vb[j] = inside ? b.y : 0.f;
-                ve[j] = static_cast<float>(static_cast<int>(__float_as_uint(fmaxf(vs[j], 5.9604645e-8f)) >> 23) - 127);
-            }
-            const bool masked = tile * 16 + 15 > len - n || n < p.n;
-            float ahead = -INFINITY;
+                for (int kt = 0; kt < KT; ++kt) {
+                    const int at = tok + 16 * kt;
+                    const unsigned char *page = st + ((at >> psh) - (tok0 >> psh)) * head_bytes;
+                    const unsigned char *codes = page + (at & (ps - 1)) * (D / 2) + lane * (D / 8);
+                    const unsigned char *pairs = page + ps * D + ((at & (ps - 1)) + g) * 4;
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float v = fmaf(ks[j], sc[nt][2 * j + e], kb[j] * qsum[nt][e]);
-                        if (masked && key0 + 8 * j > last[nt][e]) v = -INFINITY;
-                        sc[nt][2 * j + e] = v;
-                        ahead = fmaxf(ahead, v + ve[j] - m[nt][e]);
+                    for (int j = 0; j < 2; ++j) {
+                        load_codes<D>(xk[kt][j], codes + j * (4 * D));
+                        load_codes<D>(xv[kt][j], codes + ps * (D / 2) + j * (4 * D));
+                        const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(pairs + j * 32));
+                        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(pairs + ps * 4 + j * 32));
+                        ks[kt][j] = a.x * f;
+                        kb[kt][j] = (a.y - 8.f * a.x) * (f * 9.5367431640625e-7f);        // sum(q) carries no 2^-20
+                        vs[kt][j] = b.x;
+                        vb[kt][j] = b.y;
+                        if (masked && at + g + 8 * j >= len) vs[kt][j] = vb[kt][j] = 0.f;   // the rest of a page holds anything
                     }
-            // weights are taken relative to m >= max(score + exponent of s_v) - kAttendLazy
-            if (__any_sync(0xffffffffu, ahead > kAttendLazy)) {
+                }
+                // ---- scores of keys g, g + 8 against columns 2 t, 2 t + 1
+                float sc[KT][NT][4];
 #pragma unroll
-                for (int nt = 0; nt < NT; ++nt)
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        float top = fmaxf(sc[nt][e] + ve[0], sc[nt][2 + e] + ve[1]);
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                        for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                        const float now = fmaxf(m[nt][e], top);
-                        const float by = exp2_approx(m[nt][e] - now);
-                        m[nt][e] = now;
-                        l[nt][e] *= by;
-                        ob[nt][e] *= by;
+                        for (int j = 0; j < 4; ++j) sc[kt][nt][j] = 0.f;
 #pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            acc[nt][i][e] *= by;
-                            acc[nt][i][2 + e] *= by;
+                for (int w = 0; w < W; ++w) {
+#pragma unroll
+                    for (int kt = 0; kt < KT; ++kt) {
+                        uint32_t a[4], b[4];
+                        unpack4(xk[kt][0].w[w], a);
+                        unpack4(xk[kt][1].w[w], b);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            uint4 q4;
+                            if (QREG) q4 = make_uint4(qf[QREG ? nt : 0][w][0], qf[QREG ? nt : 0][w][1], qf[QREG ? nt : 0][w][2], qf[QREG ? nt : 0][w][3]);
+                            else q4 = q_smem[(nt * W + w) * 32 + lane];
+                            mma_f16(sc[kt][nt], a[0], b[0], a[1], b[1], q4.x, q4.y);
+                            mma_f16(sc[kt][nt], a[2], b[2], a[3], b[3], q4.z, q4.w);
                         }
                     }
-            }
-            uint32_t pf[NT][2];
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const float p0 = exp2_approx(sc[nt][2 * j] - (m[nt][0] - kAttendBias));
-                    const float p1 = exp2_approx(sc[nt][2 * j + 1] - (m[nt][1] - kAttendBias));
-                    l[nt][0] += p0;
-                    l[nt][1] += p1;
-                    ob[nt][0] = fmaf(p0, vb[j], ob[nt][0]);
-                    ob[nt][1] = fmaf(p1, vb[j], ob[nt][1]);
-                    const __half2 h = __floats2half2_rn(p0 * vs[j], p1 * vs[j]);
-                    pf[nt][j] = transpose8x8(*reinterpret_cast<const uint32_t *>(&h));
                 }
-            // ---- output rows (dimensions) 16 i + g, 16 i + 8 + g
+                float pr[KT][NT][4];
+                float ahead = -INFINITY, v_top = 0.f;
 #pragma unroll
-            for (int w = 0; w < W / 2; ++w) {                        // words of a token's D / 16 bytes
+                for (int kt = 0; kt < KT; ++kt) {
+                    v_top = fmaxf(v_top, fmaxf(vs[kt][0], vs[kt][1]));
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t a[4], b[4];
-                    const uint32_t pick = half ? 0x7632 : 0x5410;
-                    unpack4(__byte_perm(x.v[0].w[w], x.v[0].w[W / 2 + w], pick), a);
-                    unpack4(__byte_perm(x.v[1].w[w], x.v[1].w[W / 2 + w], pick), b);
+                    for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) {
-                        mma_f16(acc[nt][4 * w + 2 * half], a[0], a[1], b[0], b[1], pf[nt][0], pf[nt][1]);
-                        mma_f16(acc[nt][4 * w + 2 * half + 1], a[2], a[3], b[2], b[3], pf[nt][0], pf[nt][1]);
+                        for (int j = 0; j < 2; ++j)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                float v = fmaf(ks[kt][j], sc[kt][nt][2 * j + e], fmaf(kb[kt][j], qsum[nt][e], -mb[nt][e]));
+                                if (masked && tok + 16 * kt + g + 8 * j > last[nt][e]) v = -INFINITY;
+                                pr[kt][nt][2 * j + e] = v;
+                                ahead = fmaxf(ahead, v);
+                            }
+                }
+                if (__any_sync(0xffffffffu, ahead > kAttendLazy + kAttendBias || v_top >= v_limit)) {
+                    // a new maximum, or V scales beyond the unit: bring the sums to the new reference
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, o));
+                    float ratio = 1.f;
+                    if (v_top >= v_limit && v_top > 0.f) {
+                        const int e = static_cast<int>(__float_as_uint(v_top) >> 23) - 127;   // fp16: -24 .. 15
+                        const float unit = __uint_as_float((127 - e) << 23);
+                        ratio = unit / v_unit;
+                        v_unit = unit;
+                        v_limit = __uint_as_float((127 + e + 1) << 23);
                     }
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+                            float top = -INFINITY;
+#pragma unroll
+                            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) {
+                                    float v = fmaf(ks[kt][j], sc[kt][nt][2 * j + e], kb[kt][j] * qsum[nt][e]);
+                                    if (masked && tok + 16 * kt + g + 8 * j > last[nt][e]) v = -INFINITY;
+                                    pr[kt][nt][2 * j + e] = v;
+                                    top = fmaxf(top, v);
+                                }
+                            top -= kAttendBias;
+#pragma unroll
+                            for (int o = 4; o < 32; o <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+                            const float now = fmaxf(mb[nt][e], top);
+                            const float by = exp2_approx(mb[nt][e] - now);
+                            mb[nt][e] = now;
+                            l[nt][e] *= by;
+                            ob[nt][e] *= by;
+                            const float by_acc = by * ratio;
+#pragma unroll
+                            for (int i = 0; i < MT; ++i) {
+                                acc[nt][i][e] *= by_acc;
+                                acc[nt][i][2 + e] *= by_acc;
+                            }
+#pragma unroll
+                            for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                                for (int j = 0; j < 2; ++j) pr[kt][nt][2 * j + e] -= now;
+                        }
                 }
+                uint32_t pf[KT][NT][2];
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float vu = vs[kt][j] * v_unit;
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            const float p0 = exp2_approx(pr[kt][nt][2 * j]), p1 = exp2_approx(pr[kt][nt][2 * j + 1]);
+                            l[nt][0] += p0;
+                            l[nt][1] += p1;
+                            ob[nt][0] = fmaf(p0, vb[kt][j], ob[nt][0]);
+                            ob[nt][1] = fmaf(p1, vb[kt][j], ob[nt][1]);
+                            const __half2 hp = __floats2half2_rn(p0 * vu, p1 * vu);
+                            pf[kt][nt][j] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hp));
+                        }
+                    }
+                // ---- output rows (dimensions) 16 i + g, 16 i + 8 + g
+#pragma unroll
+                for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+                    for (int w = 0; w < W / 2; ++w) {                    // words of a token's D / 16 bytes
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            uint32_t a[4], b[4];
+                            const uint32_t pick = half ? 0x7632 : 0x5410;
+                            const uint32_t xa = __byte_perm(xv[kt][0].w[w], xv[kt][0].w[W / 2 + w], pick);
+                            const uint32_t xb = __byte_perm(xv[kt][1].w[w], xv[kt][1].w[W / 2 + w], pick);
+                            if (NT == 1) unpack4(xa, a), unpack4(xb, b);
+                            else unpack4_centred(xa, a), unpack4_centred(xb, b);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                mma_f16(acc[nt][4 * w + 2 * half], a[0], a[1], b[0], b[1], pf[kt][nt][0], pf[kt][nt][1]);
+                                mma_f16(acc[nt][4 * w + 2 * half + 1], a[2], a[3], b[2], b[3], pf[kt][nt][0], pf[kt][nt][1]);
+                            }
+                            if (NT == 1) {
+                                mma_f16(acc[0][4 * w + 2 * half], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pf[kt][0][0], pf[kt][0][1]);
+                                mma_f16(acc[0][4 * w + 2 * half + 1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pf[kt][0][0], pf[kt][0][1]);
+                            }
+                        }
+                    }
+            };
+            const int tiles = (min(unit_tokens, len - tok0) + 15) >> 4;
+#pragma unroll 1
+            for (int h = 0; h < tiles; h += KT) {
+                if (tok0 + 16 * (h + KT) - 1 > len - n || n < p.n) tile(std::true_type{}, h);
+                else tile(std::false_type{}, h);
             }
+            __syncwarp();                // the stage has been read: it may be overwritten
+            issue();
+            slot = slot + 1 == STAGES ? 0 : slot + 1;
+            parity ^= slot == 0;
         }
 
         // ---- the piece is done: sums over the lanes that share a column
@@ -380,8 +627,9 @@ attend_kernel(const AttendParams p) {
                     l[nt][e] += __shfl_xor_sync(0xffffffffu, l[nt][e], o);
                     ob[nt][e] += __shfl_xor_sync(0xffffffffu, ob[nt][e], o);
                 }
-        const bool whole = seg.tile == 0 && tiles == seg.tiles;
-        const int slot = 2 * worker + (seg.tile == 0 ? 1 : 0);
+        const bool whole = mine == seg.units;
+        const int64_t piece = 2 * worker + (seg.unit == 0 ? 1 : 0);
+        const float v_back = 1.f / v_unit, lo_back = 16777216.f * v_back, hi_back = 1048576.f * v_back;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -392,57 +640,79 @@ attend_kernel(const AttendParams p) {
                     const float inv = l[nt][e] > 0.f ? 1.f / l[nt][e] : l[nt][e] == 0.f ? 0.f : NAN;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        attend_store<T>(p, seg, qr, 16 * i + g, (acc[nt][i][e] + ob[nt][e]) * inv);
-                        attend_store<T>(p, seg, qr, 16 * i + 8 + g, (acc[nt][i][2 + e] + ob[nt][e]) * inv);
+                        attend_store<T>(p, seg, qr, 16 * i + g, fmaf(acc[nt][i][e], lo_back, ob[nt][e]) * inv);
+                        attend_store<T>(p, seg, qr, 16 * i + 8 + g, fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]) * inv);
                     }
                 } else {
-                    float *o = p.part + (static_cast<int64_t>(slot) * ROWS + lr) * D;
+                    float *o = p.part + (piece * ROWS + lr) * D;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        o[16 * i + g] = acc[nt][i][e] + ob[nt][e];
-                        o[16 * i + 8 + g] = acc[nt][i][2 + e] + ob[nt][e];
+                        o[16 * i + g] = fmaf(acc[nt][i][e], lo_back, ob[nt][e]);
+                        o[16 * i + 8 + g] = fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]);
                     }
                     if (g == 0) {
-                        p.part_ml[(static_cast<int64_t>(slot) * ROWS + lr) * 2] = m[nt][e];
-                        p.part_ml[(static_cast<int64_t>(slot) * ROWS + lr) * 2 + 1] = l[nt][e];
+                        p.part_ml[(piece * ROWS + lr) * 2] = mb[nt][e];
+                        p.part_ml[(piece * ROWS + lr) * 2 + 1] = l[nt][e];
                     }
                 }
             }
-        unit += tiles;
+        seg.unit += mine;
+        if (seg.unit == seg.units) attend_next(p, cum, seg);
+        if (!QREG) __syncwarp();
     }
 }
 
-// Joins the pieces of segments that several workers shared: one CTA of D threads per segment and query row.
+// Joins the pieces of segments that several workers shared: one CTA per segment and query row. It is
+// launched before the attention kernel has ended and waits for it after its own preparations.
 template <typename T, int D, int ROWS>
-__global__ void __launch_bounds__(D)
+__global__ void __launch_bounds__(kJoinThreads)
 attend_join_kernel(const AttendParams p) {
-    extern __shared__ int attend_smem[];
-    __shared__ int scratch[32];
-    const Share share = attend_share(p, attend_smem, scratch);
+    extern __shared__ __align__(128) unsigned char attend_smem[];
+    __shared__ __align__(8) int scratch[64];
+    __shared__ float buf[32];
+    __shared__ float weight[kJoinThreads];
+    __shared__ float sums[kJoinThreads];
+    int *cum = reinterpret_cast<int *>(attend_smem);
+    const Share share = attend_share(p, cum, scratch);
+    const int tid = threadIdx.x;
     const int rows = p.n * p.group;
     const int lr = blockIdx.y;
-    // segment number -> its first unit
     const int per = p.kv.heads * p.row_blocks;
-    const int b = blockIdx.x / per, which = blockIdx.x % per;
+    const int b = blockIdx.x / per, which = blockIdx.x - b * per;
     Segment s;
     s.b = b;
     s.h = which / p.row_blocks;
-    s.rb = which % p.row_blocks;
-    s.tiles = attend_smem[b + 1] - attend_smem[b];
-    const long long first = static_cast<long long>(attend_smem[b]) * per + static_cast<long long>(which) * s.tiles;
-    const int w0 = share.owner(first), w1 = share.owner(first + s.tiles - 1);
+    s.rb = which - s.h * p.row_blocks;
+    s.units = cum[b + 1] - cum[b];
+    const long long first = static_cast<long long>(cum[b]) * per + static_cast<long long>(which) * s.units;
+    const int w0 = share.owner(first), w1 = share.owner(first + s.units - 1);
     const int qr = s.rb * ROWS + lr;
     if (w0 == w1 || qr >= rows) return;
-    auto slot_of = [&](int w) { return static_cast<int64_t>(2 * w + (w == w0 ? 1 : 0)) * ROWS + lr; };
+    cudaGridDependencySynchronize();
+    auto piece = [&](int w) { return static_cast<int64_t>(2 * w + (w == w0 ? 1 : 0)) * ROWS + lr; };
     float M = -1e30f;
-    for (int w = w0; w <= w1; ++w) M = fmaxf(M, p.part_ml[slot_of(w) * 2]);
+    for (int w = w0 + tid; w <= w1; w += kJoinThreads) M = fmaxf(M, p.part_ml[piece(w) * 2]);
+    M = block_reduce(M, buf, [](float x, float y) { return fmaxf(x, y); });
+    const int d = tid % D, lane_group = tid / D;
     float L = 0.f, o = 0.f;
-    for (int w = w0; w <= w1; ++w) {
-        const float by = exp2_approx(p.part_ml[slot_of(w) * 2] - M);
-        L = fmaf(p.part_ml[slot_of(w) * 2 + 1], by, L);
-        o = fmaf(p.part[slot_of(w) * D + threadIdx.x], by, o);
+    for (int base = w0; base <= w1; base += kJoinThreads) {
+        const int w = base + tid;
+        __syncthreads();
+        if (w <= w1) {
+            weight[tid] = exp2_approx(p.part_ml[piece(w) * 2] - M);
+            L = fmaf(p.part_ml[piece(w) * 2 + 1], weight[tid], L);
+        }
+        __syncthreads();
+        const int count = min(w1 - base + 1, kJoinThreads);
+#pragma unroll 8
+        for (int i = lane_group; i < count; i += kJoinThreads / D) o = fmaf(p.part[piece(base + i) * D + d], weight[i], o);
     }
-    attend_store<T>(p, s, qr, threadIdx.x, L > 0.f ? o / L : L == 0.f ? 0.f : NAN);
+    L = block_reduce(L, buf, [](float x, float y) { return x + y; });
+    sums[tid] = o;
+    __syncthreads();
+    if (tid >= D) return;
+    for (int i = 1; i < kJoinThreads / D; ++i) o += sums[tid + i * D];
+    attend_store<T>(p, s, qr, d, L > 0.f ? o / L : L == 0.f ? 0.f : NAN);
 }
 
 }  // namespace ralm

@@ -173,26 +173,47 @@ ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ra
                              : launch_tokens<__nv_bfloat16, 128>(append, k, x, sms, st);
 }
 
-// Column blocks of 8 query rows that one pass over the keys serves.
-int attend_nt(int rows) { return rows <= 8 ? 1 : rows <= 16 ? 2 : 4; }
-int attend_workers(int nt, int sms) { return sms * (nt <= 2 ? 2 : 1) * kAttendWarps; }
+// Column blocks of 8 query rows that one pass over the keys serves: up to 4, the rows evenly cut.
+int attend_nt(int64_t rows) {
+    const int64_t blocks = (rows + 31) / 32;
+    return static_cast<int>(std::max<int64_t>((rows + 8 * blocks - 1) / (8 * blocks), 1));
+}
+int attend_workers(int nt, int head_dim, int sms) { return sms * attend_warps(nt, head_dim); }
 
 template <typename T, int D, int NT>
 ralm_status_t launch_attend(AttendParams p, int sms, cudaStream_t st) {
-    const size_t smem = (p.kv.batch + 1) * sizeof(int);
-    p.workers = attend_workers(NT, sms);
+    constexpr int kThreads = attend_warps(NT, D) * 32;
+    constexpr int kRing = attend_warps(NT, D) * attend_warp_bytes(NT, D);
+    const int cum = (p.kv.batch + 1) * static_cast<int>(sizeof(int));
+    if (!allow_smem<attend_kernel<T, D, NT>>(kRing + (kAttendMaxBatch + 1) * static_cast<int>(sizeof(int)))) return RALM_ERR_CUDA;
+    p.workers = attend_workers(NT, D, sms);
     p.part = p.part_ml + static_cast<int64_t>(2) * p.workers * 8 * NT * 2;
-    attend_kernel<T, D, NT><<<p.workers / kAttendWarps, kAttendThreads, smem, st>>>(p);
+    attend_kernel<T, D, NT><<<sms, kThreads, kRing + cum, st>>>(p);
     ralm_status_t rs = launched();
     if (rs != RALM_OK) return rs;
-    const dim3 grid(static_cast<unsigned>(p.kv.batch) * p.kv.heads * p.row_blocks, std::min(8 * NT, p.n * p.group));
-    attend_join_kernel<T, D, 8 * NT><<<grid, D, smem, st>>>(p);
-    return launched();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(p.kv.batch) * p.kv.heads * p.row_blocks, std::min(8 * NT, p.n * p.group));
+    cfg.blockDim = dim3(kJoinThreads);
+    cfg.dynamicSmemBytes = cum;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D, 8 * NT>, p) != cudaSuccess) {
+        cudaGetLastError();
+        return RALM_ERR_CUDA;
+    }
+    return RALM_OK;
 }
 template <typename T, int D>
 ralm_status_t launch_attend(const AttendParams &p, int nt, int sms, cudaStream_t st) {
-    if (nt == 1) return launch_attend<T, D, 1>(p, sms, st);
-    if (nt == 2) return launch_attend<T, D, 2>(p, sms, st);
+    switch (nt) {
+        case 1: return launch_attend<T, D, 1>(p, sms, st);
+        case 2: return launch_attend<T, D, 2>(p, sms, st);
+        case 3: return launch_attend<T, D, 3>(p, sms, st);
+    }
     return launch_attend<T, D, 4>(p, sms, st);
 }
 
@@ -349,8 +370,8 @@ ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_
 int64_t ralm_kv_attend_workspace(int32_t kv_heads, int32_t head_dim, int32_t q_heads, int32_t n) {
     if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads != 0 || n < 0 || (head_dim != 64 && head_dim != 128)) return 0;
     const int64_t rows = static_cast<int64_t>(q_heads / kv_heads) * n;
-    const int nt = attend_nt(static_cast<int>(std::min<int64_t>(rows, 1 << 20)));
-    return static_cast<int64_t>(2) * attend_workers(nt, std::max(sm_count(), 1)) * 8 * nt * (head_dim + 2) * sizeof(float);
+    const int nt = attend_nt(rows);
+    return static_cast<int64_t>(2) * attend_workers(nt, head_dim, std::max(sm_count(), 1)) * 8 * nt * (head_dim + 2) * sizeof(float);
 }
 
 ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_attend_t *a, void *stream) {
@@ -369,7 +390,7 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
     if (a->workspace_bytes < ralm_kv_attend_workspace(cache->kv_heads, cache->head_dim, a->q_heads, a->n)) return RALM_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return RALM_ERR_CUDA;
-    const int nt = attend_nt(static_cast<int>(rows));
+    const int nt = attend_nt(rows);
     AttendParams p;
     p.kv = kv_params(*cache, layer, a->rows, a->batch);
     p.q = a->q;
@@ -386,6 +407,7 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
     p.row_blocks = static_cast<int>((rows + 8 * nt - 1) / (8 * nt));
     p.scale = a->scale * kLog2e;
     p.part_ml = static_cast<float *>(a->workspace);
+    p.page_shift = pg.page_size == 16 ? 4 : pg.page_size == 32 ? 5 : 6;
     p.vec = aligned16(a->q) && a->q_stride_b % 8 == 0 && a->q_stride_n % 8 == 0 && a->q_stride_h % 8 == 0;
     if (static_cast<int64_t>(a->batch) * cache->kv_heads * p.row_blocks >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
