@@ -1,4 +1,5 @@
-"""Compile the CUDA library in-tree: paper_2401_14021_b200/libralm.so (sm_100a only).
+"""Compile the CUDA library in-tree: paper_2401_14021_b200/libralm.so (sm_100a only), and beside it the
+tensor marshalling _native.so.
 
 `--debug` builds libralm_debug.so beside it with -DRALM_DEBUG_BOUNDS: every index into a global
 array that a scan kernel computes is checked against the array's extent (a violation is recorded
@@ -12,6 +13,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libralm.so")
 DEBUG_LIB = os.path.join(HERE, "libralm_debug.so")
+BINDING = os.path.join(HERE, "_native.so")      # tensor marshalling of the generator's operators
 SOURCES = ["ralm_api.cu", "generate_api.cu", "os3.cpp"]
 HEADERS = ["common.cuh", "scan.cuh", "aux_kernels.cuh", os.path.join("..", "..", "include", "ralm.h")]
 
@@ -24,6 +26,8 @@ def _newest_source_mtime() -> float:
 
 def build(force: bool = False, verbose: bool = False, debug: bool = False) -> str:
     lib = DEBUG_LIB if debug else LIB
+    if not debug:
+        build_binding(force)
     if not force and os.path.exists(lib) and os.path.getmtime(lib) >= _newest_source_mtime():
         return lib
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
@@ -38,6 +42,28 @@ def build(force: bool = False, verbose: bool = False, debug: bool = False) -> st
     subprocess.run(cmd, check=True)
     os.replace(tmp, lib)
     return lib
+
+
+def build_binding(force: bool = False) -> str:
+    """Compile csrc/binding.cpp against the installed torch: paper_2401_14021_b200/_native.so."""
+    source = os.path.join(CSRC, "binding.cpp")
+    newest = max(os.path.getmtime(p) for p in (source, os.path.join(CSRC, "..", "..", "include", "ralm.h")))
+    if not force and os.path.exists(BINDING) and os.path.getmtime(BINDING) >= newest:
+        return BINDING
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cuda = os.path.dirname(os.path.dirname(os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")))
+    include = [os.path.join(root, "include"), os.path.join(root, "include", "torch", "csrc", "api", "include"),
+               os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]
+    tmp = BINDING + ".tmp.%d" % os.getpid()
+    subprocess.run(["g++", "-O2", "-std=c++17", "-shared", "-fPIC",
+                    "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI), source, "-o", tmp]
+                   + ["-isystem" + i for i in include]
+                   + ["-L" + os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-lc10_cuda"], check=True)
+    os.replace(tmp, BINDING)
+    return BINDING
 
 
 if __name__ == "__main__":

@@ -73,21 +73,27 @@ ralm_status_t launch_cluster(void (*kernel)(Params), int rows, int cluster, int 
     return RALM_OK;
 }
 
-constexpr int kMixMaxStage = 160 * 1024;   // bytes of a row slice that a CTA keeps in shared memory
+// A row is cut over a cluster so that a slice is about 32 KB (four CTAs then fit an SM, and one CTA's
+// stores overlap another's loads), and further while there are fewer CTAs than the GPU can hold; but not
+// below two vectors per thread, where the exchange between CTAs costs more than the slices save.
+constexpr int kMixSlice = 32 * 1024;
+constexpr int kMixMaxStage = 160 * 1024;   // bytes of a slice that a CTA keeps in shared memory
 
 template <typename T>
 ralm_status_t launch_mix(MixParams p, int R, int sms, cudaStream_t st) {
     constexpr int64_t kVec = MixVec<T>::n;
     int cluster = 1;
     auto slice_of = [&](int c) { return ((p.V + kVec - 1 + c - 1) / c + kVec - 1) / kVec * kVec; };
-    while (cluster < kMixMaxCluster && (static_cast<int64_t>(R) * cluster < 4LL * sms || slice_of(cluster) * sizeof(T) > 64 * 1024) &&
-           slice_of(2 * cluster) >= 2 * kMixThreads)
+    while (cluster < kMixMaxCluster &&
+           (slice_of(cluster) * sizeof(T) > kMixSlice || (static_cast<int64_t>(R) * cluster < 4LL * sms && slice_of(2 * cluster) >= 2 * kVec * kMixThreads)))
         cluster *= 2;
     p.slice = static_cast<int>(slice_of(cluster));
-    const size_t bytes = p.slice * sizeof(T);
-    if (bytes <= kMixMaxStage && !allow_smem<mix_kernel<T, true>>(kMixMaxStage)) return RALM_ERR_CUDA;
-    if (bytes <= kMixMaxStage) return launch_cluster(mix_kernel<T, true>, R, cluster, kMixThreads, bytes, st, p);
-    return launch_cluster(mix_kernel<T, false>, R, cluster, kMixThreads, 0, st, p);
+    p.slots = 1;
+    while (p.slots < 2 * p.k) p.slots *= 2;
+    const size_t hash = p.k > 0 ? p.slots * 16 : 0, bytes = p.slice * sizeof(T);
+    if (bytes > kMixMaxStage) return launch_cluster(mix_kernel<T, false>, R, cluster, kMixThreads, hash, st, p);
+    if (!allow_smem<mix_kernel<T, true>>(kMixMaxStage + 32 * RALM_MAX_K)) return RALM_ERR_CUDA;
+    return launch_cluster(mix_kernel<T, true>, R, cluster, kMixThreads, bytes + hash, st, p);
 }
 
 bool pages_ok(const ralm_pages_t *p) {
@@ -283,8 +289,9 @@ ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft
     p.V = V;
     p.tokens = tokens;
     p.accepted = accepted;
+    // cut over a cluster while that adds CTAs that the GPU can hold at once
     int cluster = 1;
-    while (cluster < kVtMaxCluster && static_cast<int64_t>(R) * cluster < 4LL * sms && V / (2 * cluster) >= 2 * kVtThreads) cluster *= 2;
+    while (cluster < kVtMaxCluster && static_cast<int64_t>(R) * cluster < 2LL * sms && V / (2 * cluster) >= 2 * kVtThreads) cluster *= 2;
     p.slice = (V + cluster - 1) / cluster;
     return launch_cluster(verify_tokens_kernel, R, cluster, kVtThreads, 0, static_cast<cudaStream_t>(stream), p);
 }

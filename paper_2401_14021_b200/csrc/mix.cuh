@@ -26,7 +26,7 @@ __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162f
 __device__ __forceinline__ float to_float(float x) { return x; }
 
 constexpr int kMixThreads = 512;
-constexpr int kMixSlots = 2048;     // hash slots for the neighbours' tokens, twice RALM_MAX_K
+constexpr int kMixWarps = kMixThreads / 32;
 constexpr int kMixMaxCluster = 8;
 
 struct MixParams {
@@ -44,6 +44,7 @@ struct MixParams {
     float *probs;
     int64_t ld_probs;
     int slice;           // elements of a row that one CTA of the cluster handles, a multiple of 16
+    int slots;           // hash slots for the neighbours' tokens, a power of two, at least 2 k
 };
 
 template <typename T> struct MixVec {
@@ -51,7 +52,7 @@ template <typename T> struct MixVec {
     union { uint4 raw; T x[n]; };
 };
 
-// The sum of a value over the CTA; every thread gets it. `buf`: 32 floats.
+// A value reduced over the CTA; every thread gets it. `buf`: 32 floats.
 template <typename Op>
 __device__ __forceinline__ float block_reduce(float v, float *buf, Op op) {
 #pragma unroll
@@ -63,39 +64,85 @@ __device__ __forceinline__ float block_reduce(float v, float *buf, Op op) {
     for (int i = 1; i < (int)(blockDim.x >> 5); ++i) r = op(r, buf[i]);
     return r;
 }
+__device__ __forceinline__ float warp_max(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    return v;
+}
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+}
+// (m, s) stands for s 2^(m scale); s of m = -inf is 0, or NaN, and is kept as it is.
+__device__ __forceinline__ float rescaled(float m, float s, float to, float scale) {
+    return m == -INFINITY ? s : s * exp2_approx((m - to) * scale);
+}
 
 // One cluster per row; CTA c of it handles elements [c * slice, (c + 1) * slice) of the row, counted
-// from the 16-byte boundary at or below the row's start, so that 16-byte loads stay aligned for any
-// row pitch. STAGED keeps the slice in shared memory between the two passes.
+// from the 16-byte boundary at or below the row's start, so that 16-byte accesses stay aligned for any
+// row pitch. STAGED: one bulk copy brings the slice into shared memory, where both passes (maximum and
+// sum; probabilities) find it, and the neighbours are looked up while it is on its way; otherwise the
+// slice does not fit and is read twice.
 //
-// Shared neighbours' weights are summed per token in a hash table whose sums are integers (54-bit
-// fixed point in three 18-bit limbs), so the result does not depend on the order of the atomics.
+// Neighbours' weights are summed per token in a hash table whose sums are integers (54-bit fixed point in
+// three 18-bit limbs), so the result does not depend on the order of the atomics.
 template <typename T, bool STAGED>
 __global__ void __launch_bounds__(kMixThreads)
 mix_kernel(const MixParams p) {
     constexpr int VEC = MixVec<T>::n;
     extern __shared__ __align__(16) unsigned char mix_smem[];
-    __shared__ int slot_token[kMixSlots];
-    __shared__ uint32_t slot_sum[3][kMixSlots];
     __shared__ float buf[32];
-    __shared__ float2 peers[kMixMaxCluster];
+    __shared__ float2 peers[kMixMaxCluster * kMixWarps];
+    __shared__ __align__(8) uint64_t bar;
     cg::cluster_group cluster = cg::this_cluster();
     const int C = cluster.num_blocks(), c = cluster.block_rank();
-    const int row = blockIdx.x / C, tid = threadIdx.x;
+    const int row = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const T *x = static_cast<const T *>(p.logits) + static_cast<int64_t>(row) * p.ld_logits;
     float *out = p.probs + static_cast<int64_t>(row) * p.ld_probs;
     const int mis = static_cast<int>(reinterpret_cast<uintptr_t>(x) / sizeof(T) % VEC);
     const int base = c * p.slice - mis;              // row element that slice position 0 holds
     const int count = min(p.slice, p.V - base);      // positions of the slice inside the row (<= 0: none)
+    const int vecs = count > 0 ? (count + VEC - 1) / VEC : 0;
     T *stage = reinterpret_cast<T *>(mix_smem);
+    uint32_t *slot_sum = reinterpret_cast<uint32_t *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // [3][slots]
+    int *slot_token = reinterpret_cast<int *>(slot_sum + 3 * p.slots);
+    auto load = [&](int v, MixVec<T> &u) {
+        const int e = base + v * VEC;
+        if (e >= 0 && e + VEC <= p.V) {
+            u.raw = *reinterpret_cast<const uint4 *>(x + e);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) u.x[j] = e + j >= 0 && e + j < p.V ? x[e + j] : T(-INFINITY);
+        }
+    };
+    if (STAGED) {
+        const int v0 = base < 0 ? 1 : 0, v1 = max(count > 0 ? (base + vecs * VEC > p.V ? vecs - 1 : vecs) : 0, v0);   // whole vectors
+        if (tid == 0) {
+            mbar_init(smem_u32(&bar), 1);
+            mbar_fence_init();
+            const uint32_t bytes = (v1 - v0) * 16;
+            if (bytes) {
+                mbar_arrive_expect_tx(smem_u32(&bar), bytes);
+                bulk_load(smem_u32(stage + v0 * VEC), x + base + v0 * VEC, bytes, smem_u32(&bar));
+            } else {
+                mbar_arrive(smem_u32(&bar));
+            }
+        }
+        if (tid < 2 && vecs > 0) {                    // the row's ragged ends
+            const int v = tid == 0 ? 0 : vecs - 1;
+            if (v < v0 || v >= v1) {
+                MixVec<T> u;
+                load(v, u);
+                *reinterpret_cast<uint4 *>(stage + v * VEC) = u.raw;
+            }
+        }
+    }
+    cluster.barrier_arrive();
 
     // the neighbours: weights relative to the best one, their sum, and the sum per token
     float mass = 0.f;
     if (p.k > 0) {
-        for (int i = tid; i < kMixSlots; i += kMixThreads) {
-            slot_token[i] = -1;
-            slot_sum[0][i] = slot_sum[1][i] = slot_sum[2][i] = 0;
-        }
         float s[2];
         int token[2];
         float best = -INFINITY;
@@ -116,6 +163,10 @@ mix_kernel(const MixParams p) {
                 }
             }
         }
+        for (int i = tid; i < p.slots; i += kMixThreads) {
+            slot_token[i] = -1;
+            slot_sum[i] = slot_sum[p.slots + i] = slot_sum[2 * p.slots + i] = 0;
+        }
         best = block_reduce(best, buf, [](float a, float b) { return fmaxf(a, b); });
         float sum = 0.f;
 #pragma unroll
@@ -125,37 +176,30 @@ mix_kernel(const MixParams p) {
             sum += w;
             const int pos = token[j] - base;
             if (pos < 0 || pos >= p.slice) continue;
-            int h = (token[j] * 0x9E3779B1u) >> 21;
-            for (;;) {
+            int h = (token[j] * 0x9E3779B1u) >> 20 & (p.slots - 1);
+            for (;;) {                                // at most k tokens in 2 k slots: there is always a free one
                 const int seen = atomicCAS(&slot_token[h], -1, token[j]);
                 if (seen == -1 || seen == token[j]) break;
-                h = (h + 1) & (kMixSlots - 1);
+                h = (h + 1) & (p.slots - 1);
             }
             const uint64_t fixed = static_cast<uint64_t>(__float2ull_rn(w * 18014398509481984.f));  // 2^54
-            atomicAdd(&slot_sum[0][h], static_cast<uint32_t>(fixed & 0x3FFFF));
-            atomicAdd(&slot_sum[1][h], static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
-            atomicAdd(&slot_sum[2][h], static_cast<uint32_t>(fixed >> 36));
+            atomicAdd(&slot_sum[h], static_cast<uint32_t>(fixed & 0x3FFFF));
+            atomicAdd(&slot_sum[p.slots + h], static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
+            atomicAdd(&slot_sum[2 * p.slots + h], static_cast<uint32_t>(fixed >> 36));
         }
         mass = block_reduce(sum, buf, [](float a, float b) { return a + b; });
+    } else if (STAGED) {
+        __syncthreads();                              // the barrier and the ragged ends
     }
 
     // the logits: running maximum and sum
     float m = -INFINITY, s = 0.f;
-    const int vecs = count > 0 ? (count + VEC - 1) / VEC : 0;
-    auto load = [&](int v, MixVec<T> &u) {
-        const int e = base + v * VEC;
-        if (e >= 0 && e + VEC <= p.V) {
-            u.raw = *reinterpret_cast<const uint4 *>(x + e);
-        } else {
-#pragma unroll
-            for (int j = 0; j < VEC; ++j) u.x[j] = e + j >= 0 && e + j < p.V ? x[e + j] : T(-INFINITY);
-        }
-    };
+    if (STAGED && !mbar_wait_bounded(smem_u32(&bar), 0)) m = NAN;   // never seen: the row says so
 #pragma unroll 4
     for (int v = tid; v < vecs; v += kMixThreads) {
         MixVec<T> u;
-        load(v, u);
-        if (STAGED) *reinterpret_cast<uint4 *>(stage + v * VEC) = u.raw;
+        if (STAGED) u.raw = *reinterpret_cast<const uint4 *>(stage + v * VEC);
+        else load(v, u);
         float mx = to_float(u.x[0]);
 #pragma unroll
         for (int j = 1; j < VEC; ++j) mx = fmaxf(mx, to_float(u.x[j]));
@@ -164,44 +208,61 @@ mix_kernel(const MixParams p) {
             m = mx;
         }
         const float ref = m == -INFINITY ? 0.f : m;
+        float part[2] = {0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) s += exp2_approx((to_float(u.x[j]) - ref) * p.logit_scale);
+        for (int j = 0; j < VEC; ++j) part[j & 1] += exp2_approx((to_float(u.x[j]) - ref) * p.logit_scale);
+        s += part[0] + part[1];
     }
-    const float cta_m = block_reduce(m, buf, [](float a, float b) { return fmaxf(a, b); });
-    const float cta_s = block_reduce(m == -INFINITY ? s : s * exp2_approx((m - cta_m) * p.logit_scale), buf,
-                                     [](float a, float b) { return a + b; });
-    cluster.sync();
-    if (tid < C) *cluster.map_shared_rank(&peers[c], tid) = make_float2(cta_m, cta_s);
+    const float wm = warp_max(m);
+    const float ws = warp_sum(rescaled(m, s, wm, p.logit_scale));
+    cluster.barrier_wait();
+    if (lane < C) *cluster.map_shared_rank(&peers[c * kMixWarps + warp], lane) = make_float2(wm, ws);
     cluster.sync();
     float M = -INFINITY, S = 0.f;
-    for (int i = 0; i < C; ++i) M = fmaxf(M, peers[i].x);
-    for (int i = 0; i < C; ++i)
-        S += peers[i].x == -INFINITY ? peers[i].y : peers[i].y * exp2_approx((peers[i].x - M) * p.logit_scale);
+    for (int i = lane; i < C * kMixWarps; i += 32) M = fmaxf(M, peers[i].x);
+    M = warp_max(M);
+    for (int i = lane; i < C * kMixWarps; i += 32) S += rescaled(peers[i].x, peers[i].y, M, p.logit_scale);
+    S = warp_sum(S);
     const float ref = M == -INFINITY ? 0.f : M;
     // a row without neighbours is the model's alone; a row whose every logit is -inf the neighbours'
     const float lambda = mass > 0.f ? (S == 0.f ? 1.f : p.lambda) : 0.f;
     const float scale = S == 0.f ? 0.f : (1.f - lambda) / S;
-    const float *end = out + p.V;
-#pragma unroll 2
-    for (int v = tid; v < vecs; v += kMixThreads) {
-        MixVec<T> u;
-        if (STAGED) u.raw = *reinterpret_cast<const uint4 *>(stage + v * VEC);
-        else load(v, u);
-        float *o = out + base + v * VEC;
-#pragma unroll
-        for (int j = 0; j < VEC; ++j)
-            if (o + j >= out && o + j < end) o[j] = exp2_approx((to_float(u.x[j]) - ref) * p.logit_scale) * scale;
+    auto prob = [&](T z) { return exp2_approx((to_float(z) - ref) * p.logit_scale) * scale; };
+    // 16-byte stores from the first aligned element of the slice's output on, whatever that is in the input
+    const int e0 = max(base, 0), e1 = min(base + p.slice, p.V);
+    if (e0 < e1) {
+        const int head = min(static_cast<int>((4 - reinterpret_cast<uintptr_t>(out + e0) / 4 % 4) % 4), e1 - e0);
+        const int quads = (e1 - e0 - head) / 4;
+        const int first = e0 + head;
+        auto value = [&](int e) { return prob(STAGED ? stage[e - base] : x[e]); };
+        if (STAGED && (first - base) % 4 == 0) {
+#pragma unroll 4
+            for (int i = tid; i < quads; i += kMixThreads) {
+                union { uint2 half; uint4 full; T x[4]; } u;
+                if (sizeof(T) == 2) u.half = *reinterpret_cast<const uint2 *>(stage + (first - base) + 4 * i);
+                else u.full = *reinterpret_cast<const uint4 *>(stage + (first - base) + 4 * i);
+                __stcs(reinterpret_cast<float4 *>(out + first) + i, make_float4(prob(u.x[0]), prob(u.x[1]), prob(u.x[2]), prob(u.x[3])));
+            }
+        } else {
+#pragma unroll 4
+            for (int i = tid; i < quads; i += kMixThreads) {
+                const int e = first + 4 * i;
+                __stcs(reinterpret_cast<float4 *>(out + first) + i, make_float4(value(e), value(e + 1), value(e + 2), value(e + 3)));
+            }
+        }
+        const int tail = first + 4 * quads;
+        if (tid < head) out[e0 + tid] = value(e0 + tid);
+        if (tid < e1 - tail) out[tail + tid] = value(tail + tid);
     }
     if (p.k > 0 && lambda > 0.f) {
         __syncthreads();
-        for (int h = tid; h < kMixSlots; h += kMixThreads) {
+        for (int h = tid; h < p.slots; h += kMixThreads) {
             const int t = slot_token[h];
             if (t < 0) continue;
-            const uint64_t fixed = (static_cast<uint64_t>(slot_sum[2][h]) << 36) +
-                                   (static_cast<uint64_t>(slot_sum[1][h]) << 18) + slot_sum[0][h];
+            const uint64_t fixed = (static_cast<uint64_t>(slot_sum[2 * p.slots + h]) << 36) +
+                                   (static_cast<uint64_t>(slot_sum[p.slots + h]) << 18) + slot_sum[h];
             const float w = __ull2float_rn(fixed) * 5.551115123125783e-17f;                          // 2^-54
-            const float z = STAGED ? to_float(stage[t - base]) : to_float(x[t]);
-            out[t] = exp2_approx((z - ref) * p.logit_scale) * scale + lambda * w / mass;
+            out[t] = prob(STAGED ? stage[t - base] : x[t]) + lambda * w / mass;
         }
     }
 }

@@ -9,6 +9,8 @@
 #include <cooperative_groups.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace ralm {
@@ -30,14 +32,20 @@ struct VerifyTokensParams {
     int32_t *accepted;           // [R]
 };
 
-// floor(2^40 min(max(x, 0), 1)), NaN counts as 0
-__device__ __forceinline__ uint64_t fixed40(float x) {
+// floor(2^40 min(max(x, 0), 1)), NaN counts as 0, as the sum of 2^20 hi and lo. Adding 8 and rounding
+// towards zero leaves floor(2^20 x) in the last bits of the word; what that cut off is treated the same way
+// at 2^-20 of the size. The constants (the words of 8 and 2^-17) stay in the sums until the end.
+struct FixedSum { uint32_t hi, lo; };
+constexpr uint32_t kFixedHi = 0x41000000u, kFixedLo = 0x37000000u;
+__device__ __forceinline__ void fixed_add(FixedSum &s, float x) {
     x = fminf(fmaxf(x, 0.f), 1.f);
-    const uint32_t bits = __float_as_uint(x);
-    const uint64_t m = static_cast<uint64_t>((bits & 0x7FFFFFu) | 0x800000u) << 17;   // x = m 2^(e - 127 - 40)
-    const int down = 127 - static_cast<int>(bits >> 23);
-    return down < 41 ? m >> down : 0;
+    const float y = __fadd_rz(x, 8.f);
+    const float rest = __fsub_rn(x, __fsub_rn(y, 8.f));      // both exact
+    s.hi += __float_as_uint(y) - kFixedHi;
+    s.lo += __float_as_uint(__fadd_rz(rest, 7.62939453125e-6f)) - kFixedLo;
 }
+__device__ __forceinline__ uint64_t fixed_total(const FixedSum &s) { return (static_cast<uint64_t>(s.hi) << 20) + s.lo; }
+constexpr int kFixedMost = 4095;                             // terms that the 32-bit sums hold
 __device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
@@ -46,7 +54,7 @@ __device__ __forceinline__ uint64_t warp_sum_u64(uint64_t v) {
 
 // One cluster per request. CTA c sums the weights of elements [c * slice, (c + 1) * slice), each warp
 // a run of its own; the sums say which run holds the drawn token, and that CTA looks for it there.
-__global__ void __launch_bounds__(kVtThreads)
+__global__ void __launch_bounds__(kVtThreads, 2)
 verify_tokens_kernel(const VerifyTokensParams p) {
     namespace cg = cooperative_groups;
     cg::cluster_group cluster = cg::this_cluster();
@@ -96,7 +104,37 @@ verify_tokens_kernel(const VerifyTokensParams p) {
             if (qrow) x = __fsub_rn(x, qrow[v]);
             if (v == gone) x = 0.f;
         }
-        return fixed40(x);
+        FixedSum s = {0, 0};
+        fixed_add(s, x);
+        return fixed_total(s);
+    };
+    // the sum over a warp's run, each lane's part; the loads of a batch are all in flight together
+    auto run_sum = [&](int w0, int w1, auto with_q) -> uint64_t {
+        constexpr bool minus_q = decltype(with_q)::value;
+        constexpr int kBatch = 8;
+        uint64_t total = 0;
+        FixedSum s = {0, 0};
+        int terms = 0, v = w0 + lane;
+        for (; v + 32 * (kBatch - 1) < w1; v += 32 * kBatch) {
+            float x[kBatch], y[kBatch];
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) x[j] = __ldcs(prow + v + 32 * j);
+            if (minus_q) {
+#pragma unroll
+                for (int j = 0; j < kBatch; ++j) y[j] = __ldcs(qrow + v + 32 * j);
+            }
+#pragma unroll
+            for (int j = 0; j < kBatch; ++j) fixed_add(s, minus_q ? __fsub_rn(x[j], y[j]) : x[j]);
+            terms += kBatch;
+            if (terms > kFixedMost - kBatch) {
+                total += fixed_total(s);
+                s = {0, 0};
+                terms = 0;
+            }
+        }
+        for (; v < w1; v += 32) fixed_add(s, minus_q ? __fsub_rn(prow[v], qrow[v]) : prow[v]);   // fewer than kBatch
+        total += fixed_total(s);
+        return total;
     };
     int64_t *out = p.tokens + static_cast<int64_t>(r) * (p.S + 1);
     if (c == 0) {
@@ -108,9 +146,10 @@ verify_tokens_kernel(const VerifyTokensParams p) {
     for (int round = 0; round < 2; ++round) {
         const bool whole = round == 1 || a >= n;
         const int w0 = min(lo + warp * run, hi), w1 = min(w0 + run, hi);
-        uint64_t sum = 0;
-#pragma unroll 8
-        for (int v = w0 + lane; v < w1; v += 32) sum += weight(v, whole);
+        uint64_t sum;
+        if (qrow && !whole) sum = run_sum(w0, w1, std::true_type{});
+        else sum = run_sum(w0, w1, std::false_type{});
+        if (!whole && gone >= w0 && gone < w1 && lane == 0) sum -= weight(static_cast<int>(gone), true);
         sum = warp_sum_u64(sum);
         if (lane == 0) warp_total[warp] = sum;
         if (round == 0) cluster.sync(); else __syncthreads();   // warp totals; every CTA of the cluster runs

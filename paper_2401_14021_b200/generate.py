@@ -1,15 +1,16 @@
 """The generator's side of the serving loop (include/ralm.h): the KNN-LM mixture, verification of
 drafted tokens, the pages of a cache, and the cache held in 4 bits with its attention.
 
-Like binding.py this only marshals arguments: torch supplies device memory and streams."""
+Like binding.py this only marshals arguments (in csrc/binding.cpp, where the checks of a call cost less
+than a kernel launch): torch supplies device memory and streams."""
 import ctypes
+import os
 
 import torch
 
-from .binding import L2, _check, _dev, _stream_ptr, load_library
+from .binding import L2, RalmError, _dev, _stream_ptr, load_library
 
-_i32, _i64, _p, _f32 = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p, ctypes.c_float
-_DTYPES = {torch.float16: 0, torch.bfloat16: 1, torch.float32: 2}
+_i32, _i64, _p = ctypes.c_int32, ctypes.c_int64, ctypes.c_void_p
 
 
 class _Pages(ctypes.Structure):
@@ -22,70 +23,30 @@ class _Kv(ctypes.Structure):
     _fields_ = [("pages", _Pages), ("kv_heads", _i32), ("head_dim", _i32)]
 
 
-class _Tokens(ctypes.Structure):
-    _fields_ = [("k", _p), ("v", _p), ("k_b", _i64), ("k_n", _i64), ("k_h", _i64), ("v_b", _i64), ("v_n", _i64),
-                ("v_h", _i64), ("batch", _i32), ("n", _i32), ("dtype", _i32), ("rows", _p), ("starts", _p),
-                ("count", _p)]
+_calls = None
 
 
-class _Attend(ctypes.Structure):
-    _fields_ = [("q", _p), ("out", _p), ("q_b", _i64), ("q_n", _i64), ("q_h", _i64), ("o_b", _i64), ("o_n", _i64),
-                ("o_h", _i64), ("batch", _i32), ("n", _i32), ("q_heads", _i32), ("dtype", _i32), ("scale", _f32),
-                ("rows", _p), ("q_len", _p), ("workspace", _p), ("workspace_bytes", _i64)]
-
-
-_declared = None
-
-
-def _lib():
-    """The library with the prototypes of this module's calls."""
-    global _declared
+def _native():
+    """The marshalling module, holding the entry points of the loaded library."""
+    global _calls
     lib = load_library()
-    if _declared is lib:
-        return lib
-    lib.ralm_knn_mix.argtypes = [_p, _i32, _i64, _i32, _i32, _p, _p, _i32, _i32, _p, _i64, _f32, _f32, _f32, _p, _i64, _p]
-    lib.ralm_verify_tokens.argtypes = [_p, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _i32, _i32, _i32, _p, _p, _p]
+    if _calls is not None and _calls[0] is lib:
+        return _calls[1]
+    path = os.path.join(os.path.dirname(os.path.abspath(__file__)), "_native.so")
+    if not os.path.exists(path):
+        raise RuntimeError("%s is missing: build it with `python -m paper_2401_14021_b200.build`" % path)
+    from . import _native as module
+    names = ("ralm_knn_mix", "ralm_verify_tokens", "ralm_pages_resize", "ralm_pages_fork", "ralm_pages_compact",
+             "ralm_pages_copy", "ralm_kv_append", "ralm_kv_read", "ralm_kv_attend")
+    module.bind({name: ctypes.cast(getattr(lib, name), _p).value for name in names}, RalmError)
     lib.ralm_pages_workspace.argtypes = [_i32]
     lib.ralm_pages_workspace.restype = _i64
-    lib.ralm_pages_resize.argtypes = [_p, _p, _p]
-    lib.ralm_pages_fork.argtypes = [_p, _p, _p, _i32, _p]
-    lib.ralm_pages_compact.argtypes = [_p, _p, _p]
-    lib.ralm_pages_copy.argtypes = [_p, _p, _p, _p, _i32, _p]
     lib.ralm_pages_status.argtypes = [_p, _p]
-    lib.ralm_kv_append.argtypes = [_p, _i32, _p, _p]
-    lib.ralm_kv_read.argtypes = [_p, _i32, _p, _p]
+    lib.ralm_pages_status.restype = _i32
     lib.ralm_kv_attend_workspace.argtypes = [_i32, _i32, _i32, _i32]
     lib.ralm_kv_attend_workspace.restype = _i64
-    lib.ralm_kv_attend.argtypes = [_p, _i32, _p, _p]
-    for name in ("ralm_knn_mix", "ralm_verify_tokens", "ralm_pages_resize", "ralm_pages_fork", "ralm_pages_compact",
-                 "ralm_pages_copy", "ralm_pages_status", "ralm_kv_append", "ralm_kv_read", "ralm_kv_attend"):
-        getattr(lib, name).restype = _i32
-    _declared = lib
-    return lib
-
-
-def _shape(t: torch.Tensor, shape, name: str):
-    if tuple(t.shape) != tuple(shape):
-        raise TypeError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
-
-
-def _rows_of(t: torch.Tensor, dtypes, name: str) -> int:
-    """Data pointer of a CUDA tensor whose last dimension is contiguous."""
-    if not t.is_cuda or t.dtype not in dtypes or (t.shape[-1] > 1 and t.stride(-1) != 1):
-        raise TypeError("%s must be a CUDA tensor of %s with a contiguous last dimension" % (name, dtypes))
-    return t.data_ptr()
-
-
-def _ints(t, n: int, name: str) -> int:
-    if t is None:
-        return 0
-    _shape(t, (n,), name)
-    return _dev(t, torch.int32, name)
-
-
-_ANY = (torch.float16, torch.bfloat16, torch.float32)
-_HALF = (torch.float16, torch.bfloat16)
-_F32 = (torch.float32,)
+    _calls = (lib, module)
+    return module
 
 
 def knn_mix(logits: torch.Tensor, ids: torch.Tensor, scores: torch.Tensor, values: torch.Tensor, lam: float,
@@ -94,23 +55,8 @@ def knn_mix(logits: torch.Tensor, ids: torch.Tensor, scores: torch.Tensor, value
     """ralm_knn_mix: logits [R][V] (fp16, bf16 or fp32, any row pitch), the ids int64 [R][k] and scores
     fp32 [R][k] that `search` returned, values int32 [N] -> probs fp32 [R][V]. Without neighbours
     (ids = scores = values = None) it is softmax(logits / temperature)."""
-    lib = _lib()
-    R, V = logits.shape
-    lp = _rows_of(logits, _ANY, "logits")
-    if probs is None:
-        probs = torch.empty((R, V), dtype=torch.float32, device=logits.device)
-    _shape(probs, (R, V), "probs")
-    pp = _rows_of(probs, _F32, "probs")
-    k = N = ip = sp = vp = 0
-    if ids is not None:
-        k, N = ids.shape[1], values.shape[0]
-        _shape(ids, (R, k), "ids")
-        _shape(scores, (R, k), "scores")
-        ip, sp, vp = _dev(ids, torch.int64, "ids"), _dev(scores, torch.float32, "scores"), _dev(values, torch.int32, "values")
-    _check(lib.ralm_knn_mix(lp, _DTYPES[logits.dtype], logits.stride(0) if R > 1 else V, R, V, ip, sp, k, metric, vp, N,
-                            lam, temperature, knn_temperature, pp, probs.stride(0) if R > 1 else V,
-                            _stream_ptr(stream)), "ralm_knn_mix")
-    return probs
+    return (_calls[1] if _calls else _native()).knn_mix(logits, ids, scores, values, lam, temperature, knn_temperature,
+                                                        metric, probs, stream)
 
 
 def verify_tokens(draft_tokens: torch.Tensor, draft_probs, target_probs: torch.Tensor, uniforms: torch.Tensor,
@@ -118,26 +64,13 @@ def verify_tokens(draft_tokens: torch.Tensor, draft_probs, target_probs: torch.T
     """ralm_verify_tokens: draft_tokens int64 [R][S], draft_probs fp32 [R][S][V] or None (drafts that came
     with certainty), target_probs fp32 [R][S + 1][V], uniforms fp32 [R][S + 1], draft_len int32 [R] or
     None -> (tokens int64 [R][S + 1], accepted int32 [R])."""
-    lib = _lib()
-    R, S = draft_tokens.shape
-    V = target_probs.shape[2]
-    _shape(target_probs, (R, S + 1, V), "target_probs")
-    _shape(uniforms, (R, S + 1), "uniforms")
-    tp = _rows_of(target_probs, _F32, "target_probs")
-    dp = d0 = d1 = 0
-    if draft_probs is not None:
-        _shape(draft_probs, (R, S, V), "draft_probs")
-        dp, d0, d1 = _rows_of(draft_probs, _F32, "draft_probs"), draft_probs.stride(0), draft_probs.stride(1)
-    if tokens is None:
-        tokens = torch.empty((R, S + 1), dtype=torch.int64, device=target_probs.device)
-    if accepted is None:
-        accepted = torch.empty((R,), dtype=torch.int32, device=target_probs.device)
-    _shape(tokens, (R, S + 1), "tokens")
-    _check(lib.ralm_verify_tokens(_dev(draft_tokens, torch.int64, "draft_tokens"), dp, d0, d1, tp, target_probs.stride(0),
-                                  target_probs.stride(1), _dev(uniforms, torch.float32, "uniforms"),
-                                  _ints(draft_len, R, "draft_len"), R, S, V, _dev(tokens, torch.int64, "tokens"),
-                                  _ints(accepted, R, "accepted"), _stream_ptr(stream)), "ralm_verify_tokens")
-    return tokens, accepted
+    return (_calls[1] if _calls else _native()).verify_tokens(draft_tokens, draft_probs, target_probs, uniforms,
+                                                              draft_len, tokens, accepted, stream)
+
+
+def _shape(t: torch.Tensor, shape, name: str):
+    if tuple(t.shape) != tuple(shape):
+        raise TypeError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(t.shape)))
 
 
 class Pages:
@@ -147,7 +80,8 @@ class Pages:
     lengths = refs = 0, which `Pages.allocate` makes. To be used from one stream at a time."""
 
     def __init__(self, pool, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, page_size: int):
-        self._lib = _lib()
+        self._call = _native()
+        self._lib = load_library()
         rows, max_pages = table.shape
         pages = refs.shape[0]
         _shape(lengths, (rows,), "lengths")
@@ -180,25 +114,19 @@ class Pages:
 
     def resize(self, new_lengths: torch.Tensor, stream=None):
         """ralm_pages_resize: give back, copy on write and take pages for new_lengths int32 [rows]."""
-        _check(self._lib.ralm_pages_resize(self._ptr, _ints(new_lengths, self._c.rows, "new_lengths"), _stream_ptr(stream)),
-               "ralm_pages_resize")
+        self._call.pages_resize(self._ptr, new_lengths, stream)
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
         """ralm_pages_fork: rows dst int32 [n] come to hold the pages of rows src int32 [n]."""
-        n = src.shape[0]
-        _check(self._lib.ralm_pages_fork(self._ptr, _ints(src, n, "src"), _ints(dst, n, "dst"), n, _stream_ptr(stream)),
-               "ralm_pages_fork")
+        self._call.pages_fork(self._ptr, src, dst, stream)
 
     def compact(self, stream=None) -> torch.Tensor:
         """ralm_pages_compact: live pages become 0 .. live - 1; returns live, int32 [1] on the device."""
-        _check(self._lib.ralm_pages_compact(self._ptr, self.live.data_ptr(), _stream_ptr(stream)), "ralm_pages_compact")
-        return self.live
+        return self._call.pages_compact(self._ptr, self.live, stream)
 
     def copy_from(self, other: "Pages", src: torch.Tensor, dst: torch.Tensor, stream=None):
         """ralm_pages_copy: contents of `other`'s pages src int32 [n] into this pool's pages dst int32 [n]."""
-        n = src.shape[0]
-        _check(self._lib.ralm_pages_copy(other._ptr, _ints(src, n, "src"), self._ptr, _ints(dst, n, "dst"), n,
-                                         _stream_ptr(stream)), "ralm_pages_copy")
+        self._call.pages_copy(other._ptr, src, self._ptr, dst, stream)
 
     def device_status(self, stream=None) -> int:
         """ralm_pages_status: reads and clears the status word (synchronises)."""
@@ -219,7 +147,8 @@ class KVCache(Pages):
         self.kv_heads, self.head_dim = kv_heads, head_dim
         self._kv = _Kv(pages=self._c, kv_heads=kv_heads, head_dim=head_dim)
         self._kv_ptr = ctypes.addressof(self._kv)
-        self._attend_work = {}
+        self._scale = head_dim ** -0.5
+        self._attend_work = {}      # (queries, heads) -> workspace
 
     @staticmethod
     def page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
@@ -231,60 +160,42 @@ class KVCache(Pages):
         return cls(*cls.tensors(layers, pages, cls.page_bytes(kv_heads, head_dim, page_size), rows, max_pages, device),
                    kv_heads=kv_heads, head_dim=head_dim, page_size=page_size)
 
-    def _tokens(self, k, v, starts, count, rows):
-        if k.dim() != 4 or k.shape[2] != self.kv_heads or k.shape[3] != self.head_dim or k.dtype != v.dtype:
-            raise TypeError("k and v must be [batch][n][%d][%d] of one type" % (self.kv_heads, self.head_dim))
-        _shape(v, k.shape, "v")
-        batch, n = k.shape[:2]
-        if rows is None and batch > self._c.rows:
-            raise TypeError("more entries than rows of the table")
-        return _Tokens(_rows_of(k, _HALF, "k"), _rows_of(v, _HALF, "v"), *k.stride()[:3], *v.stride()[:3], batch, n,
-                       _DTYPES[k.dtype], _ints(rows, batch, "rows"), _ints(starts, batch, "starts"),
-                       _ints(count, batch, "count"))
-
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, count: torch.Tensor = None,
                rows: torch.Tensor = None, stream=None):
         """ralm_kv_append: k, v [batch][n][kv_heads][head_dim] (fp16 or bf16) into positions starts
         int32 [batch] and on, below the rows' lengths."""
-        t = self._tokens(k, v, starts, count, rows)
-        _check(self._lib.ralm_kv_append(self._kv_ptr, layer, ctypes.addressof(t), _stream_ptr(stream)), "ralm_kv_append")
+        self._call.kv_append(self._kv_ptr, layer, k, v, starts, count, rows, stream)
 
     def read(self, layer: int, starts: torch.Tensor, n: int, dtype=torch.float16, k: torch.Tensor = None,
              v: torch.Tensor = None, count: torch.Tensor = None, rows: torch.Tensor = None, stream=None):
         """ralm_kv_read: the values of positions starts .. starts + n - 1 -> (k, v) [batch][n][kv_heads][head_dim]."""
-        shape = (starts.shape[0], n, self.kv_heads, self.head_dim)
-        if k is None:
-            k = torch.empty(shape, dtype=dtype, device=starts.device)
-        if v is None:
-            v = torch.empty(shape, dtype=k.dtype, device=starts.device)
-        _shape(k, shape, "k")
-        t = self._tokens(k, v, starts, count, rows)
-        _check(self._lib.ralm_kv_read(self._kv_ptr, layer, ctypes.addressof(t), _stream_ptr(stream)), "ralm_kv_read")
-        return k, v
+        if k is None or v is None:
+            shape = (starts.shape[0], n, self.kv_heads, self.head_dim)
+            k = torch.empty(shape, dtype=dtype, device=starts.device) if k is None else k
+            v = torch.empty(shape, dtype=k.dtype, device=starts.device) if v is None else v
+        if k.dim() != 4 or k.shape[1] != n:
+            raise TypeError("k must be [batch][%d][kv_heads][head_dim]" % n)
+        return self._call.kv_read(self._kv_ptr, layer, k, v, starts, count, rows, stream)
 
     def attend(self, layer: int, q: torch.Tensor, scale: float = None, q_len: torch.Tensor = None,
                rows: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:
         """ralm_kv_attend: q [batch][n][q_heads][head_dim], the rows' newest n tokens -> out, the same shape
         and type. scale defaults to head_dim ** -0.5."""
-        if q.dim() != 4 or q.shape[3] != self.head_dim:
-            raise TypeError("q must be [batch][n][q_heads][%d]" % self.head_dim)
-        batch, n, heads = q.shape[:3]
-        if rows is None and batch > self._c.rows:
-            raise TypeError("more entries than rows of the table")
-        if out is None:
-            out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        _shape(out, q.shape, "out")
-        if out.dtype != q.dtype:
-            raise TypeError("out must have q's type")
-        work = self._attend_work.get((heads, n))
+        work = self._attend_work.get(q.shape[1:3])
         if work is None:
+            work = self._attend_workspace(q)
+        return self._call.kv_attend(self._kv_ptr, layer, q, self._scale if scale is None else scale, q_len, rows, out,
+                                    work, stream)
+
+    def _attend_workspace(self, q: torch.Tensor) -> torch.Tensor:
+        """Room for the partial results of split rows, kept for later calls with as many queries and heads."""
+        if q.dim() != 4:
+            raise TypeError("q must be [batch][n][q_heads][%d]" % self.head_dim)
+        n, heads = q.shape[1:3]
+        with torch.cuda.device(self.table.device):
             size = self._lib.ralm_kv_attend_workspace(self.kv_heads, self.head_dim, heads, n)
-            work = next((w for w in self._attend_work.values() if w.numel() >= size), None)
-            if work is None:
-                work = torch.empty(max(size, 16), dtype=torch.uint8, device=q.device)
-            self._attend_work[heads, n] = work
-        a = _Attend(_rows_of(q, _HALF, "q"), _rows_of(out, _HALF, "out"), *q.stride()[:3], *out.stride()[:3], batch, n, heads,
-                    _DTYPES[q.dtype], self.head_dim ** -0.5 if scale is None else scale, _ints(rows, batch, "rows"),
-                    _ints(q_len, batch, "q_len"), work.data_ptr(), work.numel())
-        _check(self._lib.ralm_kv_attend(self._kv_ptr, layer, ctypes.addressof(a), _stream_ptr(stream)), "ralm_kv_attend")
-        return out
+        work = next((w for w in self._attend_work.values() if w.numel() >= size), None)
+        if work is None:
+            work = torch.empty(max(size, 16), dtype=torch.uint8, device=self.table.device)
+        self._attend_work[q.shape[1:3]] = work
+        return work
