@@ -73,9 +73,9 @@ ralm_status_t launch_cluster(void (*kernel)(Params), int rows, int cluster, int 
     return RALM_OK;
 }
 
-// A row is cut over a cluster so that a slice is about 32 KB (four CTAs then fit an SM, and one CTA's
+// A row is cut over a cluster so that a slice is about 32 KB (six CTAs then fit an SM, and one CTA's
 // stores overlap another's loads), and further while there are fewer CTAs than the GPU can hold; but not
-// below two vectors per thread, where the exchange between CTAs costs more than the slices save.
+// below one vector per thread.
 constexpr int kMixSlice = 32 * 1024;
 constexpr int kMixMaxStage = 160 * 1024;   // bytes of a slice that a CTA keeps in shared memory
 
@@ -85,7 +85,7 @@ ralm_status_t launch_mix(MixParams p, int R, int sms, cudaStream_t st) {
     int cluster = 1;
     auto slice_of = [&](int c) { return ((p.V + kVec - 1 + c - 1) / c + kVec - 1) / kVec * kVec; };
     while (cluster < kMixMaxCluster &&
-           (slice_of(cluster) * sizeof(T) > kMixSlice || (static_cast<int64_t>(R) * cluster < 4LL * sms && slice_of(2 * cluster) >= 2 * kVec * kMixThreads)))
+           (slice_of(cluster) * sizeof(T) > kMixSlice || (static_cast<int64_t>(R) * cluster < 4LL * sms && slice_of(2 * cluster) >= kVec * kMixThreads)))
         cluster *= 2;
     p.slice = static_cast<int>(slice_of(cluster));
     p.slots = 1;

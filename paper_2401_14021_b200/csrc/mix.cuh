@@ -9,6 +9,8 @@
 #include <cuda_fp16.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "common.cuh"
 
 namespace ralm {
@@ -25,8 +27,9 @@ __device__ __forceinline__ float to_float(__half x) { return __half2float(x); }
 __device__ __forceinline__ float to_float(__nv_bfloat16 x) { return __bfloat162float(x); }
 __device__ __forceinline__ float to_float(float x) { return x; }
 
-constexpr int kMixThreads = 512;
+constexpr int kMixThreads = 256;
 constexpr int kMixWarps = kMixThreads / 32;
+constexpr int kMixNeighbours = 4;    // per thread: RALM_MAX_K / kMixThreads
 constexpr int kMixMaxCluster = 8;
 
 struct MixParams {
@@ -74,16 +77,57 @@ __device__ __forceinline__ float warp_sum(float v) {
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
-// (m, s) stands for s 2^(m scale); s of m = -inf is 0, or NaN, and is kept as it is.
-__device__ __forceinline__ float rescaled(float m, float s, float to, float scale) {
-    return m == -INFINITY ? s : s * exp2_approx((m - to) * scale);
+// What the exponentials of a row are taken relative to. In powers of two the reference is a whole number r
+// at or above the largest exponent m scale: x scale - r is then one fused product and sum, rounded once, and
+// two references differ by an exact power of two. Where m scale is too large for that (rows whose logits are
+// all the type's lowest value, infinities) the differences x - m are scaled instead.
+struct MixRef {
+    float m, r;
+    bool wide;
+    __device__ __forceinline__ MixRef(float top, float scale) : m(top), r(0.f), wide(false) {
+        if (top == -INFINITY) return;
+        const float e = top * scale;
+        wide = !(fabsf(e) < 1e18f);
+        if (!wide) r = ceilf(e);
+    }
+    __device__ __forceinline__ float power(float x, float scale) const {   // 2^(x scale) over the reference
+        return wide ? exp2_approx((x - m) * scale) : exp2_approx(fmaf(x, scale, -r));
+    }
+};
+// A sum relative to `from`, relative to `to`; one over nothing but -inf is 0 (or NaN) and stays as it is.
+__device__ __forceinline__ float rescaled(const MixRef &from, float s, const MixRef &to, float scale) {
+    if (from.m == -INFINITY) return s;
+    return s * exp2_approx(from.wide || to.wide ? (from.m - to.m) * scale : from.r - to.r);
+}
+__device__ __forceinline__ float vec_max(const MixVec<float> &u) { return fmaxf(fmaxf(u.x[0], u.x[1]), fmaxf(u.x[2], u.x[3])); }
+__device__ __forceinline__ float vec_max(const MixVec<__half> &u) {
+    const __half2 *h = reinterpret_cast<const __half2 *>(u.x);
+    const __half2 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return __half2float(__hmax(__low2half(m), __high2half(m)));
+}
+__device__ __forceinline__ float vec_max(const MixVec<__nv_bfloat16> &u) {
+    const __nv_bfloat162 *h = reinterpret_cast<const __nv_bfloat162 *>(u.x);
+    const __nv_bfloat162 m = __hmax2(__hmax2(h[0], h[1]), __hmax2(h[2], h[3]));
+    return __bfloat162float(__hmax(__low2bfloat16(m), __high2bfloat16(m)));
+}
+__device__ __forceinline__ uint32_t map_to_rank(uint32_t addr, int rank) {   // the same variable in another CTA of the cluster
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+// Stores 8 bytes into another CTA's shared memory and counts them on a barrier there.
+__device__ __forceinline__ void st_async_f32x2(uint32_t addr, float a, float b, uint32_t bar) {
+    asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(addr), "f"(a), "f"(b),
+                 "r"(bar)
+                 : "memory");
 }
 
 // One cluster per row; CTA c of it handles elements [c * slice, (c + 1) * slice) of the row, counted
 // from the 16-byte boundary at or below the row's start, so that 16-byte accesses stay aligned for any
-// row pitch. STAGED: one bulk copy brings the slice into shared memory, where both passes (maximum and
-// sum; probabilities) find it, and the neighbours are looked up while it is on its way; otherwise the
-// slice does not fit and is read twice.
+// row pitch. STAGED: one bulk copy brings the slice into shared memory, where all passes (maximum; sum;
+// probabilities) find it, and the neighbours are looked up while it is on its way; otherwise the
+// slice does not fit and is read from global memory again. The CTAs exchange one (maximum, sum) per warp,
+// by stores that count on the receiver's barrier.
 //
 // Neighbours' weights are summed per token in a hash table whose sums are integers (54-bit fixed point in
 // three 18-bit limbs), so the result does not depend on the order of the atomics.
@@ -92,9 +136,9 @@ __global__ void __launch_bounds__(kMixThreads)
 mix_kernel(const MixParams p) {
     constexpr int VEC = MixVec<T>::n;
     extern __shared__ __align__(16) unsigned char mix_smem[];
-    __shared__ float buf[32];
-    __shared__ float2 peers[kMixMaxCluster * kMixWarps];
-    __shared__ __align__(8) uint64_t bar;
+    __shared__ float best_of[kMixWarps], mass_of[kMixWarps];
+    __shared__ __align__(8) float2 peers[kMixMaxCluster * kMixWarps];
+    __shared__ __align__(8) uint64_t bars[2];
     cg::cluster_group cluster = cg::this_cluster();
     const int C = cluster.num_blocks(), c = cluster.block_rank();
     const int row = blockIdx.x / C, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -104,6 +148,7 @@ mix_kernel(const MixParams p) {
     const int base = c * p.slice - mis;              // row element that slice position 0 holds
     const int count = min(p.slice, p.V - base);      // positions of the slice inside the row (<= 0: none)
     const int vecs = count > 0 ? (count + VEC - 1) / VEC : 0;
+    const uint32_t arrived = smem_u32(&bars[0]), told = smem_u32(&bars[1]);
     T *stage = reinterpret_cast<T *>(mix_smem);
     uint32_t *slot_sum = reinterpret_cast<uint32_t *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // [3][slots]
     int *slot_token = reinterpret_cast<int *>(slot_sum + 3 * p.slots);
@@ -116,61 +161,64 @@ mix_kernel(const MixParams p) {
             for (int j = 0; j < VEC; ++j) u.x[j] = e + j >= 0 && e + j < p.V ? x[e + j] : T(-INFINITY);
         }
     };
-    if (STAGED) {
-        const int v0 = base < 0 ? 1 : 0, v1 = max(count > 0 ? (base + vecs * VEC > p.V ? vecs - 1 : vecs) : 0, v0);   // whole vectors
-        if (tid == 0) {
-            mbar_init(smem_u32(&bar), 1);
-            mbar_fence_init();
+    const int v0 = base < 0 ? 1 : 0, v1 = max(vecs > 0 && base + vecs * VEC > p.V ? vecs - 1 : vecs, v0);   // whole vectors
+    if (tid == 0) {
+        mbar_init(arrived, 1);
+        mbar_init(told, 1);
+        mbar_fence_init();
+        mbar_arrive_expect_tx(told, C * kMixWarps * 8);
+        if (STAGED) {
             const uint32_t bytes = (v1 - v0) * 16;
             if (bytes) {
-                mbar_arrive_expect_tx(smem_u32(&bar), bytes);
-                bulk_load(smem_u32(stage + v0 * VEC), x + base + v0 * VEC, bytes, smem_u32(&bar));
+                mbar_arrive_expect_tx(arrived, bytes);
+                bulk_load(smem_u32(stage + v0 * VEC), x + base + v0 * VEC, bytes, arrived);
             } else {
-                mbar_arrive(smem_u32(&bar));
-            }
-        }
-        if (tid < 2 && vecs > 0) {                    // the row's ragged ends
-            const int v = tid == 0 ? 0 : vecs - 1;
-            if (v < v0 || v >= v1) {
-                MixVec<T> u;
-                load(v, u);
-                *reinterpret_cast<uint4 *>(stage + v * VEC) = u.raw;
+                mbar_arrive(arrived);
             }
         }
     }
-    cluster.barrier_arrive();
+    if (STAGED && tid < 2 && vecs > 0) {              // the row's ragged ends
+        const int v = tid == 0 ? 0 : vecs - 1;
+        if (v < v0 || v >= v1) {
+            MixVec<T> u;
+            load(v, u);
+            *reinterpret_cast<uint4 *>(stage + v * VEC) = u.raw;
+        }
+    }
+    __syncthreads();
+    asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // the barriers stand (fenced above)
 
-    // the neighbours: weights relative to the best one, their sum, and the sum per token
-    float mass = 0.f;
-    if (p.k > 0) {
-        float s[2];
-        int token[2];
+    // the neighbours, by as many warps as they fill: weights relative to the best, their sum per token
+    const int k_warps = min((p.k + 31) / 32, kMixWarps);
+    if (warp < k_warps) {
+        float s[kMixNeighbours];
+        int token[kMixNeighbours];
         float best = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const int i = tid + j * kMixThreads;
+        for (int j = 0; j < kMixNeighbours; ++j) {
+            const int i = tid + j * k_warps * 32;
             token[j] = -1;
             if (i < p.k) {
                 const int64_t id = p.ids[static_cast<int64_t>(row) * p.k + i];
-                const float sc = p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_scale;
-                if (id >= 0 && id < p.N && fabsf(sc) < INFINITY) {
-                    const int t = p.values[id];
-                    if (t >= 0 && t < p.V) {
-                        token[j] = t;
-                        s[j] = sc;
-                        best = fmaxf(best, sc);
-                    }
-                }
+                s[j] = p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_scale;
+                if (id >= 0 && id < p.N && fabsf(s[j]) < INFINITY) token[j] = p.values[id];
+                if (token[j] >= p.V) token[j] = -1;
             }
         }
-        for (int i = tid; i < p.slots; i += kMixThreads) {
+        for (int i = tid; i < p.slots; i += k_warps * 32) {
             slot_token[i] = -1;
             slot_sum[i] = slot_sum[p.slots + i] = slot_sum[2 * p.slots + i] = 0;
         }
-        best = block_reduce(best, buf, [](float a, float b) { return fmaxf(a, b); });
+#pragma unroll
+        for (int j = 0; j < kMixNeighbours; ++j)
+            if (token[j] >= 0) best = fmaxf(best, s[j]);
+        best = warp_max(best);
+        if (lane == 0) best_of[warp] = best;
+        named_barrier(1, k_warps * 32);
+        for (int i = 0; i < k_warps; ++i) best = fmaxf(best, best_of[i]);
         float sum = 0.f;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < kMixNeighbours; ++j) {
             if (token[j] < 0) continue;
             const float w = exp2_approx(s[j] - best);
             sum += w;
@@ -187,74 +235,88 @@ mix_kernel(const MixParams p) {
             atomicAdd(&slot_sum[p.slots + h], static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
             atomicAdd(&slot_sum[2 * p.slots + h], static_cast<uint32_t>(fixed >> 36));
         }
-        mass = block_reduce(sum, buf, [](float a, float b) { return a + b; });
-    } else if (STAGED) {
-        __syncthreads();                              // the barrier and the ragged ends
+        sum = warp_sum(sum);
+        if (lane == 0) mass_of[warp] = sum;
     }
 
-    // the logits: running maximum and sum
-    float m = -INFINITY, s = 0.f;
-    if (STAGED && !mbar_wait_bounded(smem_u32(&bar), 0)) m = NAN;   // never seen: the row says so
+    // the logits: the warp's maximum, then its sum
+    bool lost = STAGED && !mbar_wait_bounded(arrived, 0);
+    float m = -INFINITY;
 #pragma unroll 4
     for (int v = tid; v < vecs; v += kMixThreads) {
         MixVec<T> u;
         if (STAGED) u.raw = *reinterpret_cast<const uint4 *>(stage + v * VEC);
         else load(v, u);
-        float mx = to_float(u.x[0]);
-#pragma unroll
-        for (int j = 1; j < VEC; ++j) mx = fmaxf(mx, to_float(u.x[j]));
-        if (mx > m) {
-            s *= exp2_approx((m - mx) * p.logit_scale);   // m = -inf: s is 0 (or NaN) and stays it
-            m = mx;
-        }
-        const float ref = m == -INFINITY ? 0.f : m;
+        m = fmaxf(m, vec_max(u));
+    }
+    const MixRef mine(warp_max(m), p.logit_scale);
+    float s = lost ? NAN : 0.f;                       // never seen: the row says so
+#pragma unroll 4
+    for (int v = tid; v < vecs; v += kMixThreads) {
+        MixVec<T> u;
+        if (STAGED) u.raw = *reinterpret_cast<const uint4 *>(stage + v * VEC);
+        else load(v, u);
         float part[2] = {0.f, 0.f};
+        if (mine.wide) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) part[j & 1] += exp2_approx((to_float(u.x[j]) - ref) * p.logit_scale);
+            for (int j = 0; j < VEC; ++j) part[j & 1] += exp2_approx((to_float(u.x[j]) - mine.m) * p.logit_scale);
+        } else {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) part[j & 1] += exp2_approx(fmaf(to_float(u.x[j]), p.logit_scale, -mine.r));
+        }
         s += part[0] + part[1];
     }
-    const float wm = warp_max(m);
-    const float ws = warp_sum(rescaled(m, s, wm, p.logit_scale));
-    cluster.barrier_wait();
-    if (lane < C) *cluster.map_shared_rank(&peers[c * kMixWarps + warp], lane) = make_float2(wm, ws);
-    cluster.sync();
-    float M = -INFINITY, S = 0.f;
+    s = warp_sum(s);
+    asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
+    if (lane < C) st_async_f32x2(map_to_rank(smem_u32(&peers[c * kMixWarps + warp]), lane), mine.m, s, map_to_rank(told, lane));
+    __syncthreads();                                  // the neighbours' sums
+    lost = !mbar_wait_bounded(told, 0);
+    float M = -INFINITY, S = lost ? NAN : 0.f;
     for (int i = lane; i < C * kMixWarps; i += 32) M = fmaxf(M, peers[i].x);
-    M = warp_max(M);
-    for (int i = lane; i < C * kMixWarps; i += 32) S += rescaled(peers[i].x, peers[i].y, M, p.logit_scale);
+    const MixRef ref(warp_max(M), p.logit_scale);
+    for (int i = lane; i < C * kMixWarps; i += 32) S += rescaled(MixRef(peers[i].x, p.logit_scale), peers[i].y, ref, p.logit_scale);
     S = warp_sum(S);
-    const float ref = M == -INFINITY ? 0.f : M;
+    float mass = 0.f;
+    for (int i = 0; i < k_warps; ++i) mass += mass_of[i];
     // a row without neighbours is the model's alone; a row whose every logit is -inf the neighbours'
     const float lambda = mass > 0.f ? (S == 0.f ? 1.f : p.lambda) : 0.f;
     const float scale = S == 0.f ? 0.f : (1.f - lambda) / S;
-    auto prob = [&](T z) { return exp2_approx((to_float(z) - ref) * p.logit_scale) * scale; };
     // 16-byte stores from the first aligned element of the slice's output on, whatever that is in the input
     const int e0 = max(base, 0), e1 = min(base + p.slice, p.V);
     if (e0 < e1) {
         const int head = min(static_cast<int>((4 - reinterpret_cast<uintptr_t>(out + e0) / 4 % 4) % 4), e1 - e0);
         const int quads = (e1 - e0 - head) / 4;
         const int first = e0 + head;
-        auto value = [&](int e) { return prob(STAGED ? stage[e - base] : x[e]); };
-        if (STAGED && (first - base) % 4 == 0) {
+        auto write = [&](auto wide_type) {
+            constexpr bool wide = decltype(wide_type)::value;
+            auto prob = [&](T z) {
+                return exp2_approx(wide ? (to_float(z) - ref.m) * p.logit_scale : fmaf(to_float(z), p.logit_scale, -ref.r)) * scale;
+            };
+            auto value = [&](int e) { return prob(STAGED ? stage[e - base] : x[e]); };
+            float4 *o = reinterpret_cast<float4 *>(out + first);
+            if (STAGED && (first - base) % 4 == 0) {
 #pragma unroll 4
-            for (int i = tid; i < quads; i += kMixThreads) {
-                union { uint2 half; uint4 full; T x[4]; } u;
-                if (sizeof(T) == 2) u.half = *reinterpret_cast<const uint2 *>(stage + (first - base) + 4 * i);
-                else u.full = *reinterpret_cast<const uint4 *>(stage + (first - base) + 4 * i);
-                __stcs(reinterpret_cast<float4 *>(out + first) + i, make_float4(prob(u.x[0]), prob(u.x[1]), prob(u.x[2]), prob(u.x[3])));
-            }
-        } else {
+                for (int i = tid; i < quads; i += kMixThreads) {
+                    union { uint2 half; uint4 full; T x[4]; } u;
+                    if (sizeof(T) == 2) u.half = *reinterpret_cast<const uint2 *>(stage + (first - base) + 4 * i);
+                    else u.full = *reinterpret_cast<const uint4 *>(stage + (first - base) + 4 * i);
+                    __stcs(o + i, make_float4(prob(u.x[0]), prob(u.x[1]), prob(u.x[2]), prob(u.x[3])));
+                }
+            } else {
 #pragma unroll 4
-            for (int i = tid; i < quads; i += kMixThreads) {
-                const int e = first + 4 * i;
-                __stcs(reinterpret_cast<float4 *>(out + first) + i, make_float4(value(e), value(e + 1), value(e + 2), value(e + 3)));
+                for (int i = tid; i < quads; i += kMixThreads) {
+                    const int e = first + 4 * i;
+                    __stcs(o + i, make_float4(value(e), value(e + 1), value(e + 2), value(e + 3)));
+                }
             }
-        }
-        const int tail = first + 4 * quads;
-        if (tid < head) out[e0 + tid] = value(e0 + tid);
-        if (tid < e1 - tail) out[tail + tid] = value(tail + tid);
+            const int tail = first + 4 * quads;
+            if (tid < head) out[e0 + tid] = value(e0 + tid);
+            if (tid < e1 - tail) out[tail + tid] = value(tail + tid);
+        };
+        if (ref.wide) write(std::true_type{});
+        else write(std::false_type{});
     }
-    if (p.k > 0 && lambda > 0.f) {
+    if (lambda > 0.f) {
         __syncthreads();
         for (int h = tid; h < p.slots; h += kMixThreads) {
             const int t = slot_token[h];
@@ -262,7 +324,7 @@ mix_kernel(const MixParams p) {
             const uint64_t fixed = (static_cast<uint64_t>(slot_sum[2 * p.slots + h]) << 36) +
                                    (static_cast<uint64_t>(slot_sum[p.slots + h]) << 18) + slot_sum[h];
             const float w = __ull2float_rn(fixed) * 5.551115123125783e-17f;                          // 2^-54
-            out[t] = prob(STAGED ? stage[t - base] : x[t]) + lambda * w / mass;
+            out[t] = ref.power(to_float(STAGED ? stage[t - base] : x[t]), p.logit_scale) * scale + lambda * w / mass;
         }
     }
 }
