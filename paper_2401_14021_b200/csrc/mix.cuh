@@ -150,8 +150,7 @@ mix_kernel(const MixParams p) {
     const int vecs = count > 0 ? (count + VEC - 1) / VEC : 0;
     const uint32_t arrived = smem_u32(&bars[0]), told = smem_u32(&bars[1]);
     T *stage = reinterpret_cast<T *>(mix_smem);
-    uint32_t *slot_sum = reinterpret_cast<uint32_t *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // [3][slots]
-    int *slot_token = reinterpret_cast<int *>(slot_sum + 3 * p.slots);
+    uint4 *slots = reinterpret_cast<uint4 *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // three limbs, token
     auto load = [&](int v, MixVec<T> &u) {
         const int e = base + v * VEC;
         if (e >= 0 && e + VEC <= p.V) {
@@ -188,55 +187,24 @@ mix_kernel(const MixParams p) {
     __syncthreads();
     asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");   // the barriers stand (fenced above)
 
-    // the neighbours, by as many warps as they fill: weights relative to the best, their sum per token
+    // the neighbours, by as many warps as they fill: what they are is asked for before the logits are worked on
     const int k_warps = min((p.k + 31) / 32, kMixWarps);
+    float score[kMixNeighbours];
+    int token[kMixNeighbours];
     if (warp < k_warps) {
-        float s[kMixNeighbours];
-        int token[kMixNeighbours];
-        float best = -INFINITY;
+        int64_t id[kMixNeighbours];
 #pragma unroll
         for (int j = 0; j < kMixNeighbours; ++j) {
             const int i = tid + j * k_warps * 32;
-            token[j] = -1;
-            if (i < p.k) {
-                const int64_t id = p.ids[static_cast<int64_t>(row) * p.k + i];
-                s[j] = p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_scale;
-                if (id >= 0 && id < p.N && fabsf(s[j]) < INFINITY) token[j] = p.values[id];
-                if (token[j] >= p.V) token[j] = -1;
-            }
+            id[j] = i < p.k ? p.ids[static_cast<int64_t>(row) * p.k + i] : -1;
+            score[j] = i < p.k ? p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_scale : 0.f;
         }
-        for (int i = tid; i < p.slots; i += k_warps * 32) {
-            slot_token[i] = -1;
-            slot_sum[i] = slot_sum[p.slots + i] = slot_sum[2 * p.slots + i] = 0;
-        }
-#pragma unroll
-        for (int j = 0; j < kMixNeighbours; ++j)
-            if (token[j] >= 0) best = fmaxf(best, s[j]);
-        best = warp_max(best);
-        if (lane == 0) best_of[warp] = best;
-        named_barrier(1, k_warps * 32);
-        for (int i = 0; i < k_warps; ++i) best = fmaxf(best, best_of[i]);
-        float sum = 0.f;
+        for (int i = tid; i < p.slots; i += k_warps * 32) slots[i] = make_uint4(0, 0, 0, 0xFFFFFFFFu);
 #pragma unroll
         for (int j = 0; j < kMixNeighbours; ++j) {
-            if (token[j] < 0) continue;
-            const float w = exp2_approx(s[j] - best);
-            sum += w;
-            const int pos = token[j] - base;
-            if (pos < 0 || pos >= p.slice) continue;
-            int h = (token[j] * 0x9E3779B1u) >> 20 & (p.slots - 1);
-            for (;;) {                                // at most k tokens in 2 k slots: there is always a free one
-                const int seen = atomicCAS(&slot_token[h], -1, token[j]);
-                if (seen == -1 || seen == token[j]) break;
-                h = (h + 1) & (p.slots - 1);
-            }
-            const uint64_t fixed = static_cast<uint64_t>(__float2ull_rn(w * 18014398509481984.f));  // 2^54
-            atomicAdd(&slot_sum[h], static_cast<uint32_t>(fixed & 0x3FFFF));
-            atomicAdd(&slot_sum[p.slots + h], static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
-            atomicAdd(&slot_sum[2 * p.slots + h], static_cast<uint32_t>(fixed >> 36));
+            token[j] = -1;
+            if (id[j] >= 0 && id[j] < p.N && fabsf(score[j]) < INFINITY) token[j] = p.values[id[j]];
         }
-        sum = warp_sum(sum);
-        if (lane == 0) mass_of[warp] = sum;
     }
 
     // the logits: the warp's maximum, then its sum
@@ -269,6 +237,43 @@ mix_kernel(const MixParams p) {
     s = warp_sum(s);
     asm volatile("barrier.cluster.wait.aligned;" ::: "memory");
     if (lane < C) st_async_f32x2(map_to_rank(smem_u32(&peers[c * kMixWarps + warp]), lane), mine.m, s, map_to_rank(told, lane));
+    // weights relative to the best neighbour, their sum, and their sums per token of the slice
+    int own[kMixNeighbours];                          // slots that this thread was the first to take
+    if (warp < k_warps) {
+        float best = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < kMixNeighbours; ++j) {
+            if (token[j] >= p.V) token[j] = -1;
+            if (token[j] >= 0) best = fmaxf(best, score[j]);
+        }
+        best = warp_max(best);
+        if (lane == 0) best_of[warp] = best;
+        named_barrier(1, k_warps * 32);
+        for (int i = 0; i < k_warps; ++i) best = fmaxf(best, best_of[i]);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < kMixNeighbours; ++j) {
+            own[j] = -1;
+            if (token[j] < 0) continue;
+            const float w = exp2_approx(score[j] - best);
+            sum += w;
+            const int pos = token[j] - base;
+            if (pos < 0 || pos >= p.slice) continue;
+            int h = (token[j] * 0x9E3779B1u) >> 20 & (p.slots - 1);
+            for (;;) {                                // at most k tokens in 2 k slots: there is always a free one
+                const uint32_t seen = atomicCAS(&slots[h].w, 0xFFFFFFFFu, static_cast<uint32_t>(token[j]));
+                if (seen == 0xFFFFFFFFu) own[j] = h;
+                if (seen == 0xFFFFFFFFu || seen == static_cast<uint32_t>(token[j])) break;
+                h = (h + 1) & (p.slots - 1);
+            }
+            const uint64_t fixed = static_cast<uint64_t>(__float2ull_rn(w * 18014398509481984.f));  // 2^54
+            atomicAdd(&slots[h].x, static_cast<uint32_t>(fixed & 0x3FFFF));
+            atomicAdd(&slots[h].y, static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
+            atomicAdd(&slots[h].z, static_cast<uint32_t>(fixed >> 36));
+        }
+        sum = warp_sum(sum);
+        if (lane == 0) mass_of[warp] = sum;
+    }
     __syncthreads();                                  // the neighbours' sums
     lost = !mbar_wait_bounded(told, 0);
     float M = -INFINITY, S = lost ? NAN : 0.f;
@@ -318,13 +323,16 @@ mix_kernel(const MixParams p) {
     }
     if (lambda > 0.f) {
         __syncthreads();
-        for (int h = tid; h < p.slots; h += kMixThreads) {
-            const int t = slot_token[h];
-            if (t < 0) continue;
-            const uint64_t fixed = (static_cast<uint64_t>(slot_sum[2 * p.slots + h]) << 36) +
-                                   (static_cast<uint64_t>(slot_sum[p.slots + h]) << 18) + slot_sum[h];
-            const float w = __ull2float_rn(fixed) * 5.551115123125783e-17f;                          // 2^-54
-            out[t] = ref.power(to_float(STAGED ? stage[t - base] : x[t]), p.logit_scale) * scale + lambda * w / mass;
+        if (warp < k_warps) {
+#pragma unroll
+            for (int j = 0; j < kMixNeighbours; ++j) {
+                if (own[j] < 0) continue;
+                const uint4 limbs = slots[own[j]];
+                const uint64_t fixed = (static_cast<uint64_t>(limbs.z) << 36) + (static_cast<uint64_t>(limbs.y) << 18) + limbs.x;
+                const float w = __ull2float_rn(fixed) * 5.551115123125783e-17f;                      // 2^-54
+                const int t = token[j];
+                out[t] = ref.power(to_float(STAGED ? stage[t - base] : x[t]), p.logit_scale) * scale + lambda * w / mass;
+            }
         }
     }
 }
