@@ -66,7 +66,6 @@ struct AttendParams {
     float *part;              // [2 * workers][8 * NT][D] partial outputs
     float *part_ml;           // [2 * workers][8 * NT][2] their maxima and sums
     int workers;
-    int page_shift;           // log2 of the page size
     int vec;                  // q is 16-byte aligned in every row
 };
 
@@ -252,7 +251,7 @@ struct AttendFeed {
         if (index >= base && index + 3 < base + 32) return;
         base = index;
         held = index + lane < p.kv.max_pages ? p.kv.table[static_cast<int64_t>(row) * p.kv.max_pages + index + lane] : 0;
-        if (index + lane < ((len - 1) >> p.page_shift) + 1 && (held < 0 || held >= p.kv.pages)) {
+        if (index + lane < ((len - 1) >> p.kv.page_shift) + 1 && (held < 0 || held >= p.kv.pages)) {
             atomicMax(p.kv.status, kStatusInvalid);
             held = 0;
         }
@@ -286,7 +285,7 @@ attend_kernel(const AttendParams p) {
     cudaTriggerProgrammaticLaunchCompletion();
     const int worker = blockIdx.x * WARPS + warp;
     if (worker >= share.workers) return;
-    const int psh = p.page_shift, ps = 1 << psh;
+    const int psh = p.kv.page_shift, ps = 1 << psh;
     const int head_bytes = ps * (D + 8);
     const int unit_tokens = 1 << share.shift;
     const int units = static_cast<int>(share.begin(worker + 1) - share.begin(worker));

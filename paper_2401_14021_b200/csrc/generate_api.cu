@@ -147,6 +147,7 @@ KvParams kv_params(const ralm_kv_t &c, int32_t layer, const int32_t *rows, int b
     k.max_pages = p.max_pages;
     k.pages = p.pages;
     k.page_size = p.page_size;
+    k.page_shift = p.page_size == 16 ? 4 : p.page_size == 32 ? 5 : 6;
     k.heads = c.kv_heads;
     k.rows = rows;
     k.batch = batch;
@@ -155,7 +156,8 @@ KvParams kv_params(const ralm_kv_t &c, int32_t layer, const int32_t *rows, int b
 
 template <typename T, int D>
 ralm_status_t launch_tokens(bool append, const KvParams &k, const KvTokens &t, int sms, cudaStream_t st) {
-    const int64_t jobs = static_cast<int64_t>(k.batch) * t.n * k.heads;
+    const int64_t jobs = static_cast<int64_t>(k.batch) * kv_blocks(t.n) * k.heads;
+    if (jobs >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
     const int blocks = static_cast<int>(std::min<int64_t>((jobs + kKvThreads / 32 - 1) / (kKvThreads / 32), 32LL * sms));
     if (append) kv_append_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
     else kv_read_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
@@ -171,7 +173,9 @@ ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ra
     if (sms == 0) return RALM_ERR_CUDA;
     const KvParams k = kv_params(*c, layer, t->rows, t->batch);
     const KvTokens x = {t->k, t->v, t->k_stride_b, t->k_stride_n, t->k_stride_h, t->v_stride_b, t->v_stride_n, t->v_stride_h,
-                        t->n, t->starts, t->count};
+                        t->n, t->starts, t->count,
+                        aligned16(t->k) && aligned16(t->v) && t->k_stride_b % 8 == 0 && t->k_stride_n % 8 == 0 &&
+                            t->k_stride_h % 8 == 0 && t->v_stride_b % 8 == 0 && t->v_stride_n % 8 == 0 && t->v_stride_h % 8 == 0};
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     if (t->dtype == RALM_F16)
         return c->head_dim == 64 ? launch_tokens<__half, 64>(append, k, x, sms, st) : launch_tokens<__half, 128>(append, k, x, sms, st);
@@ -414,7 +418,6 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
     p.row_blocks = static_cast<int>((rows + 8 * nt - 1) / (8 * nt));
     p.scale = a->scale * kLog2e;
     p.part_ml = static_cast<float *>(a->workspace);
-    p.page_shift = pg.page_size == 16 ? 4 : pg.page_size == 32 ? 5 : 6;
     p.vec = aligned16(a->q) && a->q_stride_b % 8 == 0 && a->q_stride_n % 8 == 0 && a->q_stride_h % 8 == 0;
     if (static_cast<int64_t>(a->batch) * cache->kv_heads * p.row_blocks >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
