@@ -420,8 +420,9 @@ ralm_status_t ralm_pages_compact(const ralm_pages_t *pages, int32_t *live, void 
 ralm_status_t ralm_pages_copy(const ralm_pages_t *src, const int32_t *from, const ralm_pages_t *dst,
                               const int32_t *to, int32_t n, void *stream);
 
-/* Read and clear the status word (synchronises the stream): RALM_OK, RALM_ERR_OOM,
- * RALM_ERR_INVALID_ARG. The larger one stays if several came. */
+/* Read and clear the status word (synchronises the stream): RALM_OK, RALM_ERR_INVALID_ARG, RALM_ERR_OOM or
+ * RALM_ERR_TIMEOUT (a copy of ralm_kv_attend did not arrive: its outputs are not valid, and its workspace is
+ * to be zeroed). The largest stays if several came. */
 ralm_status_t ralm_pages_status(const ralm_pages_t *pages, void *stream);
 
 /* A key-value cache held in 4 bits over such a pool: page_bytes = kv_heads * page_size * (head_dim + 8),
@@ -460,7 +461,8 @@ ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_
  * or beyond q_len, give zeros.
  *   q, out   [batch][n][q_heads][head_dim], fp16 or bf16, strides in elements, last dimension contiguous;
  *            q_heads a multiple of kv_heads, query head h reads key-value head h / (q_heads / kv_heads).
- *   workspace of ralm_kv_attend_workspace(...) bytes, 16-byte aligned; needs no initial value. */
+ *   workspace of ralm_kv_attend_workspace(...) bytes, 16-byte aligned, ZEROED by the caller before its first
+ *            use; calls of any sizes may follow one another in it, one at a time. */
 typedef struct {
     const void *q;
     void *out;

@@ -36,7 +36,6 @@ constexpr int kAttendMaxBatch = 4096;
 constexpr int kAttendStage = 64;         // tokens of a stage in shared memory, the largest unit of work
 constexpr float kAttendLazy = 6.f;       // a maximum may be this far (powers of two) behind before sums are rescaled
 constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8 + 1) is below fp16's largest
-constexpr int kJoinThreads = 256;
 
 // Warps per CTA (one CTA per SM) and whether the query operands stay in registers, by column blocks.
 __host__ __device__ constexpr int attend_warps(int nt, int d) { return nt >= 3 ? 8 : nt == 1 && d == 64 ? 16 : 12; }
@@ -63,8 +62,9 @@ struct AttendParams {
     int n, group;             // queries per entry; query heads per key-value head
     int row_blocks;           // blocks of 8 * NT query rows
     float scale;              // softmax scale * log2(e)
-    float *part;              // [2 * workers][8 * NT][D] partial outputs
-    float *part_ml;           // [2 * workers][8 * NT][2] their maxima and sums
+    float *part, *part_ml;    // per warp [2 * workers][8 * NT][D] partial outputs and [..][2] their maxima and sums
+    float *cta_part, *cta_ml; // the same per CTA
+    int *counters;            // [CTAs], zero between calls
     int workers;
     int vec;                  // q is 16-byte aligned in every row
 };
@@ -234,6 +234,167 @@ __device__ __forceinline__ void attend_store(const AttendParams &p, const Segmen
 }
 
 
+// A row's merged result: its values d of a lane's D / 32 dimensions, in units of 2^M, and the sum of weights.
+template <int D> struct RowSum {
+    float x[D / 32], M, L;
+};
+// Merges pieces first, first + stride, .. (`count` of them, the first possibly elsewhere) of one query row; a warp.
+// A piece is a row of D values and a (maximum, sum). `share`: this warp takes every `parts`-th piece, from `part` on.
+template <int D, typename Piece>
+__device__ __forceinline__ RowSum<D> attend_merge(int count, int part, int parts, Piece piece_of, const float *values, const float *ml) {
+    constexpr int E = D / 32;
+    const int lane = threadIdx.x & 31;
+    RowSum<D> r;
+    r.M = -1e30f;
+    for (int j = lane; j < count; j += 32) r.M = fmaxf(r.M, __ldcg(ml + 2 * piece_of(j)));
+    r.M = warp_max(r.M);
+    r.L = 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) r.x[e] = 0.f;
+    for (int j0 = part; j0 < count; j0 += 32 * parts) {
+        const int j = j0 + lane * parts;
+        float w = 0.f;
+        if (j < count) {
+            const float2 p = __ldcg(reinterpret_cast<const float2 *>(ml + 2 * piece_of(j)));
+            w = exp2_approx(p.x - r.M);
+            r.L = fmaf(p.y, w, r.L);
+        }
+        const int some = min(32, (count - j0 + parts - 1) / parts);
+#pragma unroll 8
+        for (int i = 0; i < some; ++i) {
+            const float wi = __shfl_sync(0xffffffffu, w, i);
+            const float *v = values + piece_of(j0 + i * parts) * D + E * lane;
+            if (E == 4) {
+                const float4 y = __ldcg(reinterpret_cast<const float4 *>(v));
+                r.x[0] = fmaf(y.x, wi, r.x[0]), r.x[1] = fmaf(y.y, wi, r.x[1]);
+                r.x[E - 2] = fmaf(y.z, wi, r.x[E - 2]), r.x[E - 1] = fmaf(y.w, wi, r.x[E - 1]);
+            } else {
+                const float2 y = __ldcg(reinterpret_cast<const float2 *>(v));
+                r.x[0] = fmaf(y.x, wi, r.x[0]), r.x[1] = fmaf(y.y, wi, r.x[1]);
+            }
+        }
+    }
+    r.L = warp_sum(r.L);
+    return r;
+}
+template <typename T, int D>
+__device__ __forceinline__ void attend_write_row(const AttendParams &p, int segment, int rows_per_block, int lr, const RowSum<D> &r) {
+    constexpr int E = D / 32;
+    const int per = p.kv.heads * p.row_blocks;
+    Segment s;
+    s.b = segment / per;
+    const int which = segment - s.b * per;
+    s.h = which / p.row_blocks;
+    s.rb = which - s.h * p.row_blocks;
+    const int row = s.rb * rows_per_block + lr;
+    if (row >= p.n * p.group) return;
+    const float inv = r.L > 0.f ? 1.f / r.L : r.L == 0.f ? 0.f : NAN;
+#pragma unroll
+    for (int e = 0; e < E; ++e) attend_store<T>(p, s, row, E * (threadIdx.x & 31) + e, r.x[e] * inv);
+}
+
+// Brings the pieces of split segments together, in two steps. Inside a CTA: the warps' shares follow one
+// another, so a segment's pieces belong to neighbouring warps; a segment that begins and ends in the CTA is
+// written, of any other one piece per CTA is left. Across CTAs: each CTA that holds a piece of a segment
+// counts itself at the segment's first CTA, and the one that finds the count complete merges (in the order of
+// the CTAs, whoever it is) and puts the count back to zero.
+//   open_piece[w]: warp w's last segment begins there and does not end: (1, segment), in piece 2 * worker + 1.
+//   left_piece[w]: warp w's first segment began before it: (1, or 2 if it ends there, segment), piece 2 * worker.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void attend_join(const AttendParams &p, const Share &share, const int *cum, int working, const int2 *open_piece,
+                                            const int2 *left_piece, float *smem) {
+    constexpr int WARPS = attend_warps(NT, D), ROWS = 8 * NT, E = D / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, cta = blockIdx.x;
+    const int rows = min(p.n * p.group, ROWS);
+    __syncthreads();
+    const bool valid = lane < working;
+    const uint32_t opens = __ballot_sync(0xffffffffu, valid && open_piece[lane < WARPS ? lane : 0].x != 0);
+    const uint32_t ends = __ballot_sync(0xffffffffu, valid && left_piece[lane < WARPS ? lane : 0].x == 2);
+    const bool carried = left_piece[0].x != 0;                         // the CTA's first segment began before it
+    const int groups = __popc(opens) + (carried ? 1 : 0);
+    bool last_open = false;                                            // a segment goes on in the next CTA
+    for (int i = warp; i < groups * rows; i += WARPS) {
+        int q = i / rows;
+        const int lr = i - q * rows;
+        const bool from_before = carried && q == 0;
+        int leader = 0;
+        if (!from_before) {
+            q -= carried ? 1 : 0;
+            uint32_t m = opens;
+            for (; q > 0; --q) m &= m - 1;
+            leader = __ffs(m) - 1;
+        }
+        const int begin = from_before ? 0 : leader + 1;                // first warp with a piece that it was left
+        const uint32_t ending = begin < 32 ? ends >> begin : 0;
+        const bool ended = ending != 0;
+        const int until = ended ? begin + __ffs(ending) : working;      // one past the last warp of the segment
+        const int count = until - begin + (from_before ? 0 : 1);
+        const int64_t worker0 = static_cast<int64_t>(cta) * WARPS;
+        auto piece_of = [&](int j) -> int64_t {
+            if (from_before) return (2 * (worker0 + j)) * ROWS + lr;
+            return (2 * (worker0 + leader + j) + (j == 0 ? 1 : 0)) * ROWS + lr;
+        };
+        const RowSum<D> r = attend_merge<D>(count, 0, 1, piece_of, p.part, p.part_ml);
+        if (!from_before && ended) {
+            attend_write_row<T, D>(p, open_piece[leader].y, ROWS, lr, r);
+        } else {
+            const int64_t at = (2LL * cta + (from_before ? 0 : 1)) * ROWS + lr;
+            float *o = p.cta_part + at * D + E * lane;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] = r.x[e];
+            if (lane == 0) *reinterpret_cast<float2 *>(p.cta_ml + 2 * at) = make_float2(r.M, r.L);
+        }
+    }
+    // the CTA's own pieces: of the segment that came in, and of the one that goes out (which may be the same)
+    const int last_leader = 31 - __clz(opens);
+    last_open = opens != 0 && (last_leader + 1 >= 32 || (ends >> (last_leader + 1)) == 0);
+    __shared__ int merge_from;
+    for (int turn = 0; turn < 2; ++turn) {
+        const bool mine = turn == 0 ? carried : last_open;
+        if (!mine) continue;                                            // the same for the whole CTA
+        const int segment = turn == 0 ? left_piece[0].y : open_piece[last_leader].y;
+        const int per = p.kv.heads * p.row_blocks;
+        const int b = segment / per, units = cum[b + 1] - cum[b];
+        const long long first = static_cast<long long>(cum[b]) * per + static_cast<long long>(segment - b * per) * units;
+        const int c0 = share.owner(first) / WARPS, c1 = share.owner(first + units - 1) / WARPS;
+        __syncthreads();
+        if (threadIdx.x == 0) {
+            __threadfence();
+            const int before = atomicAdd(&p.counters[c0], 1);
+            merge_from = before == c1 - c0 ? c0 : -1;
+            if (merge_from >= 0) p.counters[c0] = 0;
+            __threadfence();
+        }
+        __syncthreads();
+        if (merge_from < 0) continue;
+        // few rows: several warps share a row, every parts-th piece each
+        const int count = c1 - c0 + 1, parts = max(WARPS / rows, 1);
+        for (int i0 = 0; i0 < rows * parts; i0 += WARPS) {
+            const int i = i0 + warp, lr = i / parts, part = i - lr * parts;
+            const bool busy = i < rows * parts;
+            auto piece_of = [&](int j) -> int64_t { return (2LL * (c0 + j) + (j == 0 ? 1 : 0)) * ROWS + lr; };
+            RowSum<D> r;
+            if (busy) r = attend_merge<D>(count, part, parts, piece_of, p.cta_part, p.cta_ml);
+            if (parts > 1) {
+                if (busy) {
+#pragma unroll
+                    for (int e = 0; e < E; ++e) smem[warp * (D + 1) + E * lane + e] = r.x[e];
+                    if (lane == 0) smem[warp * (D + 1) + D] = r.L;
+                }
+                __syncthreads();
+                if (busy && part == 0)
+                    for (int k = 1; k < parts; ++k) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) r.x[e] += smem[(warp + k) * (D + 1) + E * lane + e];
+                        r.L += smem[(warp + k) * (D + 1) + D];
+                    }
+                __syncthreads();
+            }
+            if (busy && part == 0) attend_write_row<T, D>(p, segment, ROWS, lr, r);
+        }
+    }
+}
+
 // The stream of a worker's stages: which unit is asked for next. All lanes keep the same state except
 // `held`, where lane i holds table entry base + i of the row that is being read.
 struct AttendFeed {
@@ -272,6 +433,7 @@ attend_kernel(const AttendParams p) {
     extern __shared__ __align__(128) unsigned char attend_smem[];
     __shared__ __align__(8) int scratch[64];
     __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
+    __shared__ int2 open_piece[WARPS], left_piece[WARPS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     unsigned char *ring = attend_smem + warp * attend_warp_bytes(NT, D);
     uint4 *q_smem = reinterpret_cast<uint4 *>(ring + STAGES * STAGE);
@@ -282,18 +444,19 @@ attend_kernel(const AttendParams p) {
         mbar_fence_init();
     }
     const Share share = attend_share(p, cum, scratch);
-    cudaTriggerProgrammaticLaunchCompletion();
     const int worker = blockIdx.x * WARPS + warp;
-    if (worker >= share.workers) return;
+    const int working = min(share.workers - static_cast<int>(blockIdx.x) * WARPS, WARPS);
+    if (working <= 0) return;            // the whole CTA
+    if (lane == 0) open_piece[warp] = left_piece[warp] = make_int2(0, 0);
     const int psh = p.kv.page_shift, ps = 1 << psh;
     const int head_bytes = ps * (D + 8);
     const int unit_tokens = 1 << share.shift;
-    const int units = static_cast<int>(share.begin(worker + 1) - share.begin(worker));
+    const int units = warp < working ? static_cast<int>(share.begin(worker + 1) - share.begin(worker)) : 0;
 
     // A stage mirrors the layout of the pages that its unit lies in: page j of the unit at j * head_bytes,
     // the parts of a page at their own offsets. Half a page is four copies, a whole one is one.
     AttendFeed feed;
-    feed.seg = attend_segment(p, cum, share.begin(worker));
+    feed.seg = attend_segment(p, cum, share.begin(warp < working ? worker : static_cast<int>(blockIdx.x) * WARPS));
     feed.units_left = units;
     feed.slot = 0;
     feed.enter(p);
@@ -444,7 +607,8 @@ attend_kernel(const AttendParams p) {
                     parity ^= slot == 0;
                     mbar_wait_bounded(bar0 + 8 * slot, parity);
                 }
-                return;
+                done = units;
+                break;
             }
             ++done;
             const int tok0 = (seg.unit + u) << share.shift;
@@ -628,6 +792,11 @@ attend_kernel(const AttendParams p) {
                 }
         const bool whole = mine == seg.units;
         const int64_t piece = 2 * worker + (seg.unit == 0 ? 1 : 0);
+        if (lane == 0 && !whole) {
+            const int segment = seg.b * (p.kv.heads * p.row_blocks) + seg.h * p.row_blocks + seg.rb;
+            if (seg.unit == 0) open_piece[warp] = make_int2(1, segment);
+            else left_piece[warp] = make_int2(seg.unit + mine == seg.units ? 2 : 1, segment);
+        }
         const float v_back = 1.f / v_unit, lo_back = 16777216.f * v_back, hi_back = 1048576.f * v_back;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
@@ -659,59 +828,7 @@ attend_kernel(const AttendParams p) {
         if (seg.unit == seg.units) attend_next(p, cum, seg);
         if (!QREG) __syncwarp();
     }
-}
-
-// Joins the pieces of segments that several workers shared: one CTA per segment and query row. It is
-// launched before the attention kernel has ended and waits for it after its own preparations.
-template <typename T, int D, int ROWS>
-__global__ void __launch_bounds__(kJoinThreads)
-attend_join_kernel(const AttendParams p) {
-    extern __shared__ __align__(128) unsigned char attend_smem[];
-    __shared__ __align__(8) int scratch[64];
-    __shared__ float buf[32];
-    __shared__ float weight[kJoinThreads];
-    __shared__ float sums[kJoinThreads];
-    int *cum = reinterpret_cast<int *>(attend_smem);
-    const Share share = attend_share(p, cum, scratch);
-    const int tid = threadIdx.x;
-    const int rows = p.n * p.group;
-    const int lr = blockIdx.y;
-    const int per = p.kv.heads * p.row_blocks;
-    const int b = blockIdx.x / per, which = blockIdx.x - b * per;
-    Segment s;
-    s.b = b;
-    s.h = which / p.row_blocks;
-    s.rb = which - s.h * p.row_blocks;
-    s.units = cum[b + 1] - cum[b];
-    const long long first = static_cast<long long>(cum[b]) * per + static_cast<long long>(which) * s.units;
-    const int w0 = share.owner(first), w1 = share.owner(first + s.units - 1);
-    const int qr = s.rb * ROWS + lr;
-    if (w0 == w1 || qr >= rows) return;
-    cudaGridDependencySynchronize();
-    auto piece = [&](int w) { return static_cast<int64_t>(2 * w + (w == w0 ? 1 : 0)) * ROWS + lr; };
-    float M = -1e30f;
-    for (int w = w0 + tid; w <= w1; w += kJoinThreads) M = fmaxf(M, p.part_ml[piece(w) * 2]);
-    M = block_reduce(M, buf, [](float x, float y) { return fmaxf(x, y); });
-    const int d = tid % D, lane_group = tid / D;
-    float L = 0.f, o = 0.f;
-    for (int base = w0; base <= w1; base += kJoinThreads) {
-        const int w = base + tid;
-        __syncthreads();
-        if (w <= w1) {
-            weight[tid] = exp2_approx(p.part_ml[piece(w) * 2] - M);
-            L = fmaf(p.part_ml[piece(w) * 2 + 1], weight[tid], L);
-        }
-        __syncthreads();
-        const int count = min(w1 - base + 1, kJoinThreads);
-#pragma unroll 8
-        for (int i = lane_group; i < count; i += kJoinThreads / D) o = fmaf(p.part[piece(base + i) * D + d], weight[i], o);
-    }
-    L = block_reduce(L, buf, [](float x, float y) { return x + y; });
-    sums[tid] = o;
-    __syncthreads();
-    if (tid >= D) return;
-    for (int i = 1; i < kJoinThreads / D; ++i) o += sums[tid + i * D];
-    attend_store<T>(p, s, qr, d, L > 0.f ? o / L : L == 0.f ? 0.f : NAN);
+    attend_join<T, D, NT>(p, share, cum, working, open_piece, left_piece, reinterpret_cast<float *>(attend_smem));
 }
 
 }  // namespace ralm

@@ -188,6 +188,7 @@ int attend_nt(int64_t rows) {
     const int64_t blocks = (rows + 31) / 32;
     return static_cast<int>(std::max<int64_t>((rows + 8 * blocks - 1) / (8 * blocks), 1));
 }
+int64_t attend_counters(int sms) { return (sms + 63) / 64 * 64; }
 int attend_workers(int nt, int head_dim, int sms) { return sms * attend_warps(nt, head_dim); }
 
 template <typename T, int D, int NT>
@@ -197,25 +198,12 @@ ralm_status_t launch_attend(AttendParams p, int sms, cudaStream_t st) {
     const int cum = (p.kv.batch + 1) * static_cast<int>(sizeof(int));
     if (!allow_smem<attend_kernel<T, D, NT>>(kRing + (kAttendMaxBatch + 1) * static_cast<int>(sizeof(int)))) return RALM_ERR_CUDA;
     p.workers = attend_workers(NT, D, sms);
-    p.part = p.part_ml + static_cast<int64_t>(2) * p.workers * 8 * NT * 2;
+    p.part_ml = reinterpret_cast<float *>(p.counters + attend_counters(sms));
+    p.cta_ml = p.part_ml + static_cast<int64_t>(2) * p.workers * 8 * NT * 2;
+    p.part = p.cta_ml + static_cast<int64_t>(2) * attend_counters(sms) * 8 * NT * 2;
+    p.cta_part = p.part + static_cast<int64_t>(2) * p.workers * 8 * NT * D;
     attend_kernel<T, D, NT><<<sms, kThreads, kRing + cum, st>>>(p);
-    ralm_status_t rs = launched();
-    if (rs != RALM_OK) return rs;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(p.kv.batch) * p.kv.heads * p.row_blocks, std::min(8 * NT, p.n * p.group));
-    cfg.blockDim = dim3(kJoinThreads);
-    cfg.dynamicSmemBytes = cum;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D, 8 * NT>, p) != cudaSuccess) {
-        cudaGetLastError();
-        return RALM_ERR_CUDA;
-    }
-    return RALM_OK;
+    return launched();
 }
 template <typename T, int D>
 ralm_status_t launch_attend(const AttendParams &p, int nt, int sms, cudaStream_t st) {
@@ -295,7 +283,7 @@ ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft
     p.accepted = accepted;
     // cut over a cluster while that adds CTAs that the GPU can hold at once
     int cluster = 1;
-    while (cluster < kVtMaxCluster && static_cast<int64_t>(R) * cluster < 2LL * sms && V / (2 * cluster) >= 2 * kVtThreads) cluster *= 2;
+    while (cluster < kVtMaxCluster && 2LL * R * cluster <= 2LL * sms && V / (2 * cluster) >= 2 * kVtThreads) cluster *= 2;
     p.slice = (V + cluster - 1) / cluster;
     return launch_cluster(verify_tokens_kernel, R, cluster, kVtThreads, 0, static_cast<cudaStream_t>(stream), p);
 }
@@ -366,6 +354,7 @@ ralm_status_t ralm_pages_status(const ralm_pages_t *pages, void *stream) {
     if (cudaMemcpyAsync(&word, pages->status, sizeof(int), cudaMemcpyDeviceToHost, st) != cudaSuccess ||
         cudaMemsetAsync(pages->status, 0, sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess)
         return RALM_ERR_CUDA;
+    if (word == kStatusTimeout) return RALM_ERR_TIMEOUT;
     if (word == kStatusNoPages) return RALM_ERR_OOM;
     if (word == kStatusInvalid) return RALM_ERR_INVALID_ARG;
     return word == 0 ? RALM_OK : RALM_ERR_CUDA;
@@ -382,7 +371,9 @@ int64_t ralm_kv_attend_workspace(int32_t kv_heads, int32_t head_dim, int32_t q_h
     if (kv_heads < 1 || q_heads < kv_heads || q_heads % kv_heads != 0 || n < 0 || (head_dim != 64 && head_dim != 128)) return 0;
     const int64_t rows = static_cast<int64_t>(q_heads / kv_heads) * n;
     const int nt = attend_nt(rows);
-    return static_cast<int64_t>(2) * attend_workers(nt, head_dim, std::max(sm_count(), 1)) * 8 * nt * (head_dim + 2) * sizeof(float);
+    const int sms = std::max(sm_count(), 1);
+    return attend_counters(sms) * static_cast<int64_t>(sizeof(int)) +
+           static_cast<int64_t>(2) * (attend_workers(nt, head_dim, sms) + attend_counters(sms)) * 8 * nt * (head_dim + 2) * sizeof(float);
 }
 
 ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_attend_t *a, void *stream) {
@@ -417,7 +408,7 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
     p.group = group;
     p.row_blocks = static_cast<int>((rows + 8 * nt - 1) / (8 * nt));
     p.scale = a->scale * kLog2e;
-    p.part_ml = static_cast<float *>(a->workspace);
+    p.counters = static_cast<int *>(a->workspace);
     p.vec = aligned16(a->q) && a->q_stride_b % 8 == 0 && a->q_stride_n % 8 == 0 && a->q_stride_h % 8 == 0;
     if (static_cast<int64_t>(a->batch) * cache->kv_heads * p.row_blocks >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
     cudaStream_t st = static_cast<cudaStream_t>(stream);

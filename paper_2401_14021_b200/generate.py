@@ -160,6 +160,13 @@ class KVCache(Pages):
         return cls(*cls.tensors(layers, pages, cls.page_bytes(kv_heads, head_dim, page_size), rows, max_pages, device),
                    kv_heads=kv_heads, head_dim=head_dim, page_size=page_size)
 
+    def device_status(self, stream=None) -> int:
+        status = super().device_status(stream)
+        if status == 4:                                  # RALM_ERR_TIMEOUT: an attention call did not finish
+            for work in self._attend_work.values():
+                work.zero_()
+        return status
+
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, count: torch.Tensor = None,
                rows: torch.Tensor = None, stream=None):
         """ralm_kv_append: k, v [batch][n][kv_heads][head_dim] (fp16 or bf16) into positions starts
@@ -196,6 +203,6 @@ class KVCache(Pages):
             size = self._lib.ralm_kv_attend_workspace(self.kv_heads, self.head_dim, heads, n)
         work = next((w for w in self._attend_work.values() if w.numel() >= size), None)
         if work is None:
-            work = torch.empty(max(size, 16), dtype=torch.uint8, device=self.table.device)
+            work = torch.zeros(max(size, 16), dtype=torch.uint8, device=self.table.device)
         self._attend_work[q.shape[1:3]] = work
         return work
