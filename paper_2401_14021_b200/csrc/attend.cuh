@@ -100,6 +100,26 @@ __device__ __forceinline__ void unpack4_centred(uint32_t x, uint32_t (&y)[4]) {
     for (int i = 0; i < 4; ++i) y[i] = hsub2(y[i], i % 2 == 0 ? 0x00080008u : 0x00800080u);
 }
 
+// The largest finite absolute value of eight; infinities and NaN do not set a row's scale.
+__device__ __forceinline__ float q_top(const __half *x) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const float2 a = __half22float2(__habs2(*reinterpret_cast<const __half2 *>(x + j)));
+        top = fmaxf(top, fmaxf(a.x < INFINITY ? a.x : 0.f, a.y < INFINITY ? a.y : 0.f));
+    }
+    return top;
+}
+__device__ __forceinline__ float q_top(const __nv_bfloat16 *x) {
+    float top = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; j += 2) {
+        const float2 a = __bfloat1622float2(__habs2(*reinterpret_cast<const __nv_bfloat162 *>(x + j)));
+        top = fmaxf(top, fmaxf(a.x < INFINITY ? a.x : 0.f, a.y < INFINITY ? a.y : 0.f));
+    }
+    return top;
+}
+
 template <int D> struct LaneCodes;                                    // a lane's D / 8 bytes of a tile
 template <> struct LaneCodes<128> { union { uint4 raw; uint32_t w[4]; }; };
 template <> struct LaneCodes<64> { union { uint2 raw; uint32_t w[2]; }; };
@@ -111,12 +131,34 @@ template <int D> __device__ __forceinline__ void load_codes(LaneCodes<D> &c, con
 // one, so that an entry without keys is written too), and worker w, a warp, takes units
 // [total w / W, total (w + 1) / W): any mix of lengths is balanced to one unit. A unit is 64 tokens, or
 // 32 where there are so few that the warps would get less than two of them each.
+//
+// Where every segment is short and there are CTAs enough, a segment is given a CTA of its own instead (its
+// units cut over the CTA's warps): nothing is left to merge between CTAs, which costs more than the shares save.
 struct Share {
     long long total;
     int workers, shift;                  // log2 of a unit's tokens
-    __device__ __forceinline__ long long begin(int w) const { return total * w / workers; }
-    __device__ __forceinline__ int owner(long long u) const { return static_cast<int>(((u + 1) * workers - 1) / total); }
+    bool own_cta;                        // one CTA per segment
+    long long each, more;                // the first `more` workers take each + 1 units, the others `each`
+    __device__ __forceinline__ void cut() {
+        if (total < (1LL << 31)) {
+            const uint32_t q = static_cast<uint32_t>(total) / static_cast<uint32_t>(workers);
+            each = q;
+            more = total - static_cast<long long>(q) * workers;
+        } else {
+            each = total / workers;
+            more = total - each * workers;
+        }
+    }
+    __device__ __forceinline__ long long begin(int w) const { return each * w + min(static_cast<long long>(w), more); }
+    __device__ __forceinline__ int owner(long long u) const {
+        const long long wide = more * (each + 1);
+        if (total < (1LL << 31))
+            return u < wide ? static_cast<int>(static_cast<uint32_t>(u) / static_cast<uint32_t>(each + 1))
+                            : static_cast<int>(more) + static_cast<int>(static_cast<uint32_t>(u - wide) / static_cast<uint32_t>(each));
+        return static_cast<int>(u < wide ? u / (each + 1) : more + (u - wide) / each);
+    }
 };
+constexpr int kAttendOwnUnits = 4;       // own_cta: at most this many units of 32 tokens per warp
 // Inclusive prefix sums of the entries' units (without heads and row blocks) in shared memory: cum[b + 1]
 // for b < batch. Returns the whole.
 __device__ inline int attend_prefix(const AttendParams &p, int shift, int *cum, int *scratch) {
@@ -156,10 +198,12 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
     if (p.kv.batch <= (int)blockDim.x) {   // both cuts from one look at the lengths, packed in 64 bits
         const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
         unsigned long long units = 0;
+        bool brief = true;
         if (tid < p.kv.batch) {
             const int row = kv_row(p.kv, tid);
             const int len = row < 0 ? 0 : kv_length(p.kv, row);
             units = static_cast<unsigned long long>(max((len + 63) >> 6, 1)) << 32 | max((len + 31) >> 5, 1);
+            brief = len <= 32 * kAttendOwnUnits * static_cast<int>(blockDim.x >> 5);
         }
         unsigned long long scan = units;
 #pragma unroll
@@ -169,7 +213,7 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
         }
         unsigned long long *sums = reinterpret_cast<unsigned long long *>(scratch);
         if (lane == 31) sums[warp] = scan;
-        __syncthreads();
+        brief = __syncthreads_and(brief);
         unsigned long long before = 0, all = 0;
         const int warps = (p.kv.batch + 31) >> 5;
         for (int i = 0; i < warps; ++i) {
@@ -178,7 +222,8 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
         }
         s.shift = 6;
         s.total = static_cast<long long>(all >> 32) * per;
-        if (s.total < 2LL * p.workers) {
+        s.own_cta = brief && p.kv.batch * per <= gridDim.x;
+        if (s.own_cta || s.total < 2LL * p.workers) {
             s.shift = 5;
             s.total = static_cast<long long>(all & 0xFFFFFFFFull) * per;
         }
@@ -187,8 +232,10 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
         if (tid == 0) cum[0] = 0;
         __syncthreads();
         s.workers = static_cast<int>(min(static_cast<long long>(p.workers), s.total));
+        s.cut();
         return s;
     }
+    s.own_cta = false;
     s.shift = 6;
     s.total = attend_prefix(p, 6, cum, scratch) * per;
     if (s.total < 2LL * p.workers) {
@@ -196,6 +243,7 @@ __device__ inline Share attend_share(const AttendParams &p, int *cum, int *scrat
         s.total = attend_prefix(p, 5, cum, scratch) * per;
     }
     s.workers = static_cast<int>(min(static_cast<long long>(p.workers), s.total));
+    s.cut();
     return s;
 }
 struct Segment { int b, h, rb, unit, units; };                     // unit: place inside the segment
@@ -210,7 +258,7 @@ __device__ __forceinline__ Segment attend_segment(const AttendParams &p, const i
     s.b = lo;
     s.units = cum[lo + 1] - cum[lo];
     const long long in = unit - static_cast<long long>(cum[lo]) * per;
-    const int which = static_cast<int>(in / s.units);
+    const int which = in < (1LL << 31) ? static_cast<int>(static_cast<uint32_t>(in) / static_cast<uint32_t>(s.units)) : static_cast<int>(in / s.units);
     s.unit = static_cast<int>(in - static_cast<long long>(which) * s.units);
     s.h = which / p.row_blocks;
     s.rb = which - s.h * p.row_blocks;
@@ -225,14 +273,12 @@ __device__ __forceinline__ void attend_next(const AttendParams &p, const int *cu
     if (++s.b < p.kv.batch) s.units = cum[s.b + 1] - cum[s.b];
 }
 
-// One query row's place: query i and head of the group, from its number in the segment's entry.
+// One query row's place in the output: query i and head of the group, from its number in the segment's entry.
 template <typename T>
-__device__ __forceinline__ void attend_store(const AttendParams &p, const Segment &s, int row, int d, float x) {
-    const int i = row / p.group, gq = row % p.group;
-    T *o = static_cast<T *>(p.out) + s.b * p.o_b + i * p.o_n + (static_cast<int64_t>(s.h) * p.group + gq) * p.o_h;
-    o[d] = from_float<T>(x);
+__device__ __forceinline__ T *attend_row(const AttendParams &p, const Segment &s, int row) {
+    const int i = row / p.group, gq = row - i * p.group;
+    return static_cast<T *>(p.out) + s.b * p.o_b + i * p.o_n + (static_cast<int64_t>(s.h) * p.group + gq) * p.o_h;
 }
-
 
 // A row's merged result: its values d of a lane's D / 32 dimensions, in units of 2^M, and the sum of weights.
 template <int D> struct RowSum {
@@ -290,7 +336,7 @@ __device__ __forceinline__ void attend_write_row(const AttendParams &p, int segm
     if (row >= p.n * p.group) return;
     const float inv = r.L > 0.f ? 1.f / r.L : r.L == 0.f ? 0.f : NAN;
 #pragma unroll
-    for (int e = 0; e < E; ++e) attend_store<T>(p, s, row, E * (threadIdx.x & 31) + e, r.x[e] * inv);
+    for (int e = 0; e < E; ++e) attend_row<T>(p, s, row)[E * (threadIdx.x & 31) + e] = from_float<T>(r.x[e] * inv);
 }
 
 // Brings the pieces of split segments together, in two steps. Inside a CTA: the warps' shares follow one
@@ -445,18 +491,34 @@ attend_kernel(const AttendParams p) {
     }
     const Share share = attend_share(p, cum, scratch);
     const int worker = blockIdx.x * WARPS + warp;
-    const int working = min(share.workers - static_cast<int>(blockIdx.x) * WARPS, WARPS);
-    if (working <= 0) return;            // the whole CTA
+    Segment mine_first;                  // where the warp begins, and how many units it takes
+    int working, units;
+    if (share.own_cta) {
+        const int per = p.kv.heads * p.row_blocks, segment = blockIdx.x;
+        if (segment >= p.kv.batch * per) return;                        // the whole CTA
+        const int b = segment / per, which = segment - b * per, all = cum[b + 1] - cum[b];
+        working = min(WARPS, all);
+        mine_first.b = b;
+        mine_first.h = which / p.row_blocks;
+        mine_first.rb = which - mine_first.h * p.row_blocks;
+        mine_first.units = all;
+        mine_first.unit = all * min(warp, working) / working;
+        units = all * min(warp + 1, working) / working - mine_first.unit;
+    } else {
+        working = min(share.workers - static_cast<int>(blockIdx.x) * WARPS, WARPS);
+        if (working <= 0) return;        // the whole CTA
+        mine_first = attend_segment(p, cum, share.begin(warp < working ? worker : worker - warp));
+        units = warp < working ? static_cast<int>(share.begin(worker + 1) - share.begin(worker)) : 0;
+    }
     if (lane == 0) open_piece[warp] = left_piece[warp] = make_int2(0, 0);
     const int psh = p.kv.page_shift, ps = 1 << psh;
     const int head_bytes = ps * (D + 8);
     const int unit_tokens = 1 << share.shift;
-    const int units = warp < working ? static_cast<int>(share.begin(worker + 1) - share.begin(worker)) : 0;
 
     // A stage mirrors the layout of the pages that its unit lies in: page j of the unit at j * head_bytes,
     // the parts of a page at their own offsets. Half a page is four copies, a whole one is one.
     AttendFeed feed;
-    feed.seg = attend_segment(p, cum, share.begin(warp < working ? worker : static_cast<int>(blockIdx.x) * WARPS));
+    feed.seg = mine_first;
     feed.units_left = units;
     feed.slot = 0;
     feed.enter(p);
@@ -497,7 +559,7 @@ attend_kernel(const AttendParams p) {
             if (feed.seg.b != b) feed.enter(p);
         }
     };
-    Segment seg = feed.seg;
+    Segment seg = mine_first;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) issue();
 
@@ -518,66 +580,58 @@ attend_kernel(const AttendParams p) {
         float f = 1.f;
         {
             // bring the rows to [2^10, 2^11) by one power of two: bf16 fits fp16, and 16 q does too
-            float top = 0.f, inv = 1.f;
+            union Eight { uint4 raw; T x[8]; } u[NT][W];
+            float top = 0.f;
 #pragma unroll
-            for (int pass = 0; pass < 2; ++pass) {
-                if (pass == 1) {
+            for (int nt = 0; nt < NT; ++nt) {
+                const int qr = seg.rb * ROWS + nt * 8 + g;
+                const bool real = qr < rows;
+                const int i = real ? qr / p.group : 0, gq = real ? qr - i * p.group : 0;
+                const T *src = static_cast<const T *>(p.q) + seg.b * p.q_b + i * p.q_n +
+                               (static_cast<int64_t>(seg.h) * p.group + gq) * p.q_h + t * (D / 4);
 #pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-                    const int e = top > 0.f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 10, -100), 117) : 0;
-                    f = __uint_as_float((127 + e) << 23);
-                    inv = __uint_as_float((127 - e) << 23);
-                }
-#pragma unroll
-                for (int nt = 0; nt < NT; ++nt) {
-                    const int qr = seg.rb * ROWS + nt * 8 + g;
-                    const bool real = qr < rows;
-                    const int i = real ? qr / p.group : 0, gq = real ? qr - i * p.group : 0;
-                    const T *src = static_cast<const T *>(p.q) + seg.b * p.q_b + i * p.q_n +
-                                   (static_cast<int64_t>(seg.h) * p.group + gq) * p.q_h + t * (D / 4);
-                    float sum = 0.f;
-#pragma unroll
-                    for (int w = 0; w < W; ++w) {
-                        union { uint4 raw; T x[8]; } u;
-                        u.raw = make_uint4(0, 0, 0, 0);
-                        if (real) {
-                            if (p.vec) u.raw = *reinterpret_cast<const uint4 *>(src + 8 * w);
-                            else
-#pragma unroll
-                                for (int j = 0; j < 8; ++j) u.x[j] = src[8 * w + j];
-                        }
-                        if (pass == 0) {
-#pragma unroll
-                            for (int j = 0; j < 8; ++j) {
-                                const float x = fabsf(to_float(u.x[j]));
-                                if (x < INFINITY) top = fmaxf(top, x);
-                            }
-                            continue;
-                        }
-                        uint32_t packed[4];
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const __half2 h = __floats2half2_rn(to_float(u.x[j]) * inv, to_float(u.x[j + 4]) * inv);
-                            const float2 back = __half22float2(h);
-                            sum += back.x + back.y;
-                            const __half2 up = j % 2 == 0 ? __hmul2(h, __float2half2_rn(16.f)) : h;   // c 2^-24 against c 2^-20
-                            packed[j] = *reinterpret_cast<const uint32_t *>(&up);
-                        }
-                        if (QREG)
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) qf[QREG ? nt : 0][w][j] = packed[j];
+                for (int w = 0; w < W; ++w) {
+                    u[nt][w].raw = make_uint4(0, 0, 0, 0);
+                    if (real) {
+                        if (p.vec) u[nt][w].raw = *reinterpret_cast<const uint4 *>(src + 8 * w);
                         else
-                            q_smem[(nt * W + w) * 32 + lane] = make_uint4(packed[0], packed[1], packed[2], packed[3]);
-                    }
-                    if (pass == 0) continue;
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-                    sum += __shfl_xor_sync(0xffffffffu, sum, 2);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-                        qsum[nt][e] = __shfl_sync(0xffffffffu, sum, (2 * t + e) * 4);
-                        const int qi = (seg.rb * ROWS + nt * 8 + 2 * t + e) / p.group;
-                        last[nt][e] = qi < n ? len - n + qi : -1;
+                            for (int j = 0; j < 8; ++j) u[nt][w].x[j] = src[8 * w + j];
                     }
+                    top = fmaxf(top, q_top(u[nt][w].x));
+                }
+            }
+            top = warp_max(top);
+            const int e = top > 0.f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 10, -100), 117) : 0;
+            f = __uint_as_float((127 + e) << 23);
+            const float inv = __uint_as_float((127 - e) << 23);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float sum = 0.f;
+#pragma unroll
+                for (int w = 0; w < W; ++w) {
+                    uint32_t packed[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const __half2 h = __floats2half2_rn(to_float(u[nt][w].x[j]) * inv, to_float(u[nt][w].x[j + 4]) * inv);
+                        const float2 back = __half22float2(h);
+                        sum += back.x + back.y;
+                        const __half2 up = j % 2 == 0 ? __hmul2(h, __float2half2_rn(16.f)) : h;   // c 2^-24 against c 2^-20
+                        packed[j] = *reinterpret_cast<const uint32_t *>(&up);
+                    }
+                    if (QREG)
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) qf[QREG ? nt : 0][w][j] = packed[j];
+                    else
+                        q_smem[(nt * W + w) * 32 + lane] = make_uint4(packed[0], packed[1], packed[2], packed[3]);
+                }
+                sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+                sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    qsum[nt][c] = __shfl_sync(0xffffffffu, sum, (2 * t + c) * 4);
+                    const int qi = (seg.rb * ROWS + nt * 8 + 2 * t + c) / p.group;
+                    last[nt][c] = qi < n ? len - n + qi : -1;
                 }
             }
         }
@@ -806,10 +860,11 @@ attend_kernel(const AttendParams p) {
                 if (qr >= rows) continue;
                 if (whole) {
                     const float inv = l[nt][e] > 0.f ? 1.f / l[nt][e] : l[nt][e] == 0.f ? 0.f : NAN;
+                    T *o = attend_row<T>(p, seg, qr);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        attend_store<T>(p, seg, qr, 16 * i + g, fmaf(acc[nt][i][e], lo_back, ob[nt][e]) * inv);
-                        attend_store<T>(p, seg, qr, 16 * i + 8 + g, fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]) * inv);
+                        o[16 * i + g] = from_float<T>(fmaf(acc[nt][i][e], lo_back, ob[nt][e]) * inv);
+                        o[16 * i + 8 + g] = from_float<T>(fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]) * inv);
                     }
                 } else {
                     float *o = p.part + (piece * ROWS + lr) * D;
