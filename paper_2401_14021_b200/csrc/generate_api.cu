@@ -185,7 +185,7 @@ ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ra
 
 // Column blocks of 8 query rows that one pass over the keys serves: up to 4, the rows evenly cut.
 int attend_nt(int64_t rows) {
-    const int64_t blocks = (rows + 31) / 32;
+    const int64_t blocks = std::max<int64_t>((rows + 31) / 32, 1);
     return static_cast<int>(std::max<int64_t>((rows + 8 * blocks - 1) / (8 * blocks), 1));
 }
 int64_t attend_counters(int sms) { return (sms + 63) / 64 * 64; }

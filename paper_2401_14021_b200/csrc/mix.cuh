@@ -122,6 +122,12 @@ __device__ __forceinline__ void st_async_f32x2(uint32_t addr, float a, float b, 
                  : "memory");
 }
 
+// 2^e or 2^-e, e the exponent of a weight in (0, 1] given by its bits (0: of the smallest normal number).
+__device__ __forceinline__ float mix_unit(uint32_t bits, int sign) {
+    const int e = max(static_cast<int>(bits >> 23), 1) - 127;
+    return __uint_as_float(static_cast<uint32_t>(127 + sign * e) << 23);
+}
+
 // One cluster per row; CTA c of it handles elements [c * slice, (c + 1) * slice) of the row, counted
 // from the 16-byte boundary at or below the row's start, so that 16-byte accesses stay aligned for any
 // row pitch. STAGED: one bulk copy brings the slice into shared memory, where all passes (maximum; sum;
@@ -129,8 +135,9 @@ __device__ __forceinline__ void st_async_f32x2(uint32_t addr, float a, float b, 
 // slice does not fit and is read from global memory again. The CTAs exchange one (maximum, sum) per warp,
 // by stores that count on the receiver's barrier.
 //
-// Neighbours' weights are summed per token in a hash table whose sums are integers (54-bit fixed point in
-// three 18-bit limbs), so the result does not depend on the order of the atomics.
+// Neighbours' weights are summed per token in a hash table: first the largest weight of each token, then the
+// sum in units of 2^-41 of that one's power of two, in two limbs of 21 bits. Maxima and whole numbers have no
+// order, so the result does not depend on that of the atomics, and small sums keep their precision.
 template <typename T, bool STAGED>
 __global__ void __launch_bounds__(kMixThreads)
 mix_kernel(const MixParams p) {
@@ -150,7 +157,7 @@ mix_kernel(const MixParams p) {
     const int vecs = count > 0 ? (count + VEC - 1) / VEC : 0;
     const uint32_t arrived = smem_u32(&bars[0]), told = smem_u32(&bars[1]);
     T *stage = reinterpret_cast<T *>(mix_smem);
-    uint4 *slots = reinterpret_cast<uint4 *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // three limbs, token
+    uint4 *slots = reinterpret_cast<uint4 *>(mix_smem + (STAGED ? p.slice * sizeof(T) : 0));   // two limbs, largest weight, token
     auto load = [&](int v, MixVec<T> &u) {
         const int e = base + v * VEC;
         if (e >= 0 && e + VEC <= p.V) {
@@ -251,12 +258,13 @@ mix_kernel(const MixParams p) {
         named_barrier(1, k_warps * 32);
         for (int i = 0; i < k_warps; ++i) best = fmaxf(best, best_of[i]);
         float sum = 0.f;
+        int in_slot[kMixNeighbours];
 #pragma unroll
         for (int j = 0; j < kMixNeighbours; ++j) {
-            own[j] = -1;
+            own[j] = in_slot[j] = -1;
             if (token[j] < 0) continue;
-            const float w = exp2_approx(score[j] - best);
-            sum += w;
+            score[j] = exp2_approx(score[j] - best);  // the weight from here on
+            sum += score[j];
             const int pos = token[j] - base;
             if (pos < 0 || pos >= p.slice) continue;
             int h = (token[j] * 0x9E3779B1u) >> 20 & (p.slots - 1);
@@ -266,10 +274,17 @@ mix_kernel(const MixParams p) {
                 if (seen == 0xFFFFFFFFu || seen == static_cast<uint32_t>(token[j])) break;
                 h = (h + 1) & (p.slots - 1);
             }
-            const uint64_t fixed = static_cast<uint64_t>(__float2ull_rn(w * 18014398509481984.f));  // 2^54
-            atomicAdd(&slots[h].x, static_cast<uint32_t>(fixed & 0x3FFFF));
-            atomicAdd(&slots[h].y, static_cast<uint32_t>(fixed >> 18 & 0x3FFFF));
-            atomicAdd(&slots[h].z, static_cast<uint32_t>(fixed >> 36));
+            in_slot[j] = h;
+            atomicMax(&slots[h].z, __float_as_uint(score[j]));
+        }
+        named_barrier(1, k_warps * 32);
+#pragma unroll
+        for (int j = 0; j < kMixNeighbours; ++j) {
+            if (in_slot[j] < 0) continue;
+            uint4 &slot = slots[in_slot[j]];
+            const uint64_t fixed = __float2ull_rn(score[j] * mix_unit(slot.z, -1) * 2199023255552.f);     // 2^41
+            atomicAdd(&slot.x, static_cast<uint32_t>(fixed & 0x1FFFFF));
+            atomicAdd(&slot.y, static_cast<uint32_t>(fixed >> 21));
         }
         sum = warp_sum(sum);
         if (lane == 0) mass_of[warp] = sum;
@@ -328,8 +343,8 @@ mix_kernel(const MixParams p) {
             for (int j = 0; j < kMixNeighbours; ++j) {
                 if (own[j] < 0) continue;
                 const uint4 limbs = slots[own[j]];
-                const uint64_t fixed = (static_cast<uint64_t>(limbs.z) << 36) + (static_cast<uint64_t>(limbs.y) << 18) + limbs.x;
-                const float w = __ull2float_rn(fixed) * 5.551115123125783e-17f;                      // 2^-54
+                const uint64_t fixed = (static_cast<uint64_t>(limbs.y) << 21) + limbs.x;
+                const float w = __ull2float_rn(fixed) * 4.547473508864641e-13f * mix_unit(limbs.z, 1);   // 2^-41
                 const int t = token[j];
                 out[t] = ref.power(to_float(STAGED ? stage[t - base] : x[t]), p.logit_scale) * scale + lambda * w / mass;
             }
