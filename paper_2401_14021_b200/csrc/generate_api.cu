@@ -111,8 +111,20 @@ ralm_status_t launch_copy(const PagesCopyParams &p, int64_t most, cudaStream_t s
     if (sms == 0) return RALM_ERR_CUDA;
     const int64_t jobs = most * std::max(p.layers, 1) * ((p.page_bytes + 16383) / 16384);
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(jobs, 8LL * sms));
-    pages_copy_kernel<<<static_cast<int>(blocks), kCopyThreads, 0, st>>>(p);
-    return launched();
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(kCopyThreads);
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, pages_copy_kernel, p) != cudaSuccess) {
+        cudaGetLastError();
+        return RALM_ERR_CUDA;
+    }
+    return RALM_OK;
 }
 PagesCopyParams copy_in_pool(const ralm_pages_t &p) {
     PagesCopyParams c = {};

@@ -58,25 +58,45 @@ __device__ __forceinline__ int block_scan(int v, int *buf, int *total) {
 
 __device__ __forceinline__ bool page_ok(const ralm_pages_t &p, int page) { return page >= 0 && page < p.pages; }
 
-// lengths -> new_lengths for every row: give back, copy on write, take. One CTA; the page contents are
-// moved by pages_copy_kernel from the list that this kernel leaves in the workspace.
+constexpr int kPagesSmemList = 4096;   // free pages that the resize kernel keeps in shared memory
+
+// lengths -> new_lengths for every row: give back, copy on write, take. One CTA (the state is a few KB and each step
+// depends on the one before; what it costs is round trips to memory, so steps that no row asks for are skipped and
+// the list of free pages stays on the chip where it fits). The page contents are moved by pages_copy_kernel from
+// the list that this kernel leaves in the workspace.
 __global__ void __launch_bounds__(kPagesThreads, 1)
 pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_lengths) {
     __shared__ int buf[kPagesWarps];
-    __shared__ int bad;
+    __shared__ int near_list[kPagesSmemList];
+    __shared__ int flags;
     const PagesWork w = pages_work(p);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int ps = p.page_size, M = p.max_pages;
     const long long cap = static_cast<long long>(M) * ps;
-    if (tid == 0) bad = 0;
+    auto pages_of = [&](int length) { return (length + ps - 1) / ps; };
+    // the page that a growing row goes on writing into, or -1
+    auto last_page = [&](int r) -> int {
+        const int len = p.lengths[r];
+        return new_lengths[r] > len && len % ps != 0 ? p.table[static_cast<int64_t>(r) * M + len / ps] : -1;
+    };
+    int bad = 0, shrinks = 0, continues = 0;
+    if (tid == 0) flags = 0;
     __syncthreads();
     for (int r = tid; r < p.rows; r += kPagesThreads) {
         const int len = p.lengths[r], to = new_lengths[r];
-        if (len < 0 || len > cap || to < 0 || to > cap) bad = 1;
-        else if (to > len && len % ps != 0 && !page_ok(p, p.table[static_cast<int64_t>(r) * M + len / ps])) bad = 1;
+        if (len < 0 || len > cap || to < 0 || to > cap) {
+            bad = 1;
+        } else if (to < len) {
+            shrinks = 1;
+        } else if (to > len && len % ps != 0) {
+            continues = 1;
+            if (!page_ok(p, last_page(r))) bad = 1;
+        }
     }
+    if (bad | shrinks | continues) atomicOr(&flags, bad | shrinks << 1 | continues << 2);
     __syncthreads();
-    if (bad) {
+    const int seen = flags;
+    if (seen & 1) {
         if (tid == 0) {
             atomicMax(p.status, kStatusInvalid);
             w.head[0] = 0;
@@ -86,45 +106,51 @@ pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_length
     // give back: holders only, the table is cleared once it is known that the call goes through
     auto release = [&](int sign) {
         for (int r = warp; r < p.rows; r += kPagesWarps) {
-            const int have = (p.lengths[r] + ps - 1) / ps, need = (new_lengths[r] + ps - 1) / ps;
+            const int have = pages_of(p.lengths[r]), need = pages_of(new_lengths[r]);
             for (int c = need + lane; c < have; c += 32) {
                 const int page = p.table[static_cast<int64_t>(r) * M + c];
                 if (page_ok(p, page)) atomicAdd(&p.refs[page], sign);
             }
         }
     };
-    release(-1);
-    __syncthreads();
-    // who goes on writing into a page that others hold too
-    auto shared_page = [&](int r) -> int {
-        const int len = p.lengths[r];
-        if (new_lengths[r] <= len || len % ps == 0) return -1;
-        const int page = p.table[static_cast<int64_t>(r) * M + len / ps];
-        return p.refs[page] > 1 ? page : -1;
-    };
-    for (int r = tid; r < p.rows; r += kPagesThreads) {
-        const int page = shared_page(r);
-        if (page >= 0) {
-            atomicAdd(&w.growers[page], 1);
-            atomicMax(&w.lowest[page], p.rows - r);
-        }
+    if (seen & 2) {
+        release(-1);
+        __syncthreads();
     }
-    __syncthreads();
-    auto demand_of = [&](int r, int *cow_page) -> int {
-        const int page = shared_page(r);
-        const bool keeps = page >= 0 && w.growers[page] == p.refs[page] && w.lowest[page] == p.rows - r;
-        *cow_page = page >= 0 && !keeps ? page : -1;
-        const int have = (p.lengths[r] + ps - 1) / ps, need = (new_lengths[r] + ps - 1) / ps;
-        return max(need - have, 0) + (*cow_page >= 0);
+    // who goes on writing into a page that others hold too
+    int shared = 0;
+    if (seen & 4) {
+        for (int r = tid; r < p.rows; r += kPagesThreads) {
+            const int page = last_page(r);
+            if (page >= 0 && p.refs[page] > 1) {
+                atomicAdd(&w.growers[page], 1);
+                atomicMax(&w.lowest[page], p.rows - r);
+                shared = 1;
+            }
+        }
+        shared = __syncthreads_or(shared);
+    }
+    auto forget = [&]() {                                // the scratch counts go back to zero
+        for (int r = tid; r < p.rows; r += kPagesThreads) {
+            const int page = last_page(r);
+            if (page >= 0) w.growers[page] = w.lowest[page] = 0;
+        }
     };
+    auto copied_page = [&](int r) -> int {               // the page that the row gets a copy of, or -1
+        if (!shared) return -1;
+        const int page = last_page(r);
+        if (page < 0 || p.refs[page] <= 1) return -1;
+        return w.growers[page] == p.refs[page] && w.lowest[page] == p.rows - r ? -1 : page;
+    };
+    auto demand_of = [&](int r) { return max(pages_of(new_lengths[r]) - pages_of(p.lengths[r]), 0) + (copied_page(r) >= 0); };
     long long demand = 0;
     for (int r0 = 0; r0 < p.rows; r0 += kPagesThreads) {
-        const int r = r0 + tid;
-        int page, total;
-        block_scan(r < p.rows ? demand_of(r, &page) : 0, buf, &total);
+        int total;
+        block_scan(r0 + tid < p.rows ? demand_of(r0 + tid) : 0, buf, &total);
         demand += total;
     }
     // the lowest free pages, as many as are asked for
+    int *list = demand <= kPagesSmemList ? near_list : w.list;
     long long found = 0;
     for (int g0 = 0; g0 < p.pages && found < demand; g0 += 4 * kPagesThreads) {
         const int g = g0 + 4 * tid;
@@ -138,19 +164,13 @@ pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_length
         long long at = found + block_scan(n, buf, &total) - n;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            if (free_here[j]) w.list[at++] = g + j;
+            if (free_here[j] && at < demand) list[at++] = g + j;
         found += total;
     }
     __syncthreads();
     if (found < demand) {
-        release(+1);
-        for (int r = tid; r < p.rows; r += kPagesThreads) {
-            const int len = p.lengths[r];
-            if (new_lengths[r] > len && len % ps != 0) {
-                const int page = p.table[static_cast<int64_t>(r) * M + len / ps];
-                w.growers[page] = w.lowest[page] = 0;
-            }
-        }
+        if (seen & 2) release(+1);
+        if (shared) forget();
         if (tid == 0) {
             atomicMax(p.status, kStatusNoPages);
             w.head[0] = 0;
@@ -160,42 +180,41 @@ pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_length
     int taken = 0, moves = 0;
     for (int r0 = 0; r0 < p.rows; r0 += kPagesThreads) {
         const int r = r0 + tid;
-        int cow = -1, total, total_cow;
-        const int want = r < p.rows ? demand_of(r, &cow) : 0;
+        int total, total_copies = 0, move = moves;
+        const int copied = r < p.rows ? copied_page(r) : -1;
+        const int want = r < p.rows ? demand_of(r) : 0;
         int at = taken + block_scan(want, buf, &total) - want;
-        const int move = moves + block_scan(cow >= 0, buf, &total_cow) - (cow >= 0);
+        if (shared) move += block_scan(copied >= 0, buf, &total_copies) - (copied >= 0);
         taken += total;
-        moves += total_cow;
+        moves += total_copies;
         if (r < p.rows) {
             int32_t *row = p.table + static_cast<int64_t>(r) * M;
-            const int len = p.lengths[r], have = (len + ps - 1) / ps, need = (new_lengths[r] + ps - 1) / ps;
-            if (cow >= 0) {
-                const int page = w.list[at++];
+            const int len = p.lengths[r], have = pages_of(len), need = pages_of(new_lengths[r]);
+            if (copied >= 0) {
+                const int page = list[at++];
                 p.refs[page] = 1;
                 row[len / ps] = page;
-                w.from[move] = cow;
+                w.from[move] = copied;
                 w.to[move] = page;
             }
             for (int c = have; c < need; ++c) {
-                const int page = w.list[at++];
+                const int page = list[at++];
                 p.refs[page] = 1;
                 row[c] = page;
             }
             for (int c = need; c < have; ++c) row[c] = -1;
         }
     }
-    __syncthreads();
-    // the copied pages lose a holder; the scratch counts go back to zero
-    for (int i = tid; i < moves; i += kPagesThreads) atomicSub(&p.refs[w.from[i]], 1);
-    for (int r = tid; r < p.rows; r += kPagesThreads) {
-        const int len = p.lengths[r];
-        if (new_lengths[r] > len && len % ps != 0) {
-            const int page = p.table[static_cast<int64_t>(r) * M + len / ps];
+    if (shared) {
+        __syncthreads();
+        forget();
+        for (int i = tid; i < moves; i += kPagesThreads) {
+            const int page = w.from[i];                  // a page that was copied has a holder less
+            atomicSub(&p.refs[page], 1);
             w.growers[page] = w.lowest[page] = 0;
         }
+        __syncthreads();
     }
-    for (int i = tid; i < moves; i += kPagesThreads) w.growers[w.from[i]] = w.lowest[w.from[i]] = 0;
-    __syncthreads();
     for (int r = tid; r < p.rows; r += kPagesThreads) p.lengths[r] = new_lengths[r];
     if (tid == 0) w.head[0] = moves;
 }
@@ -318,6 +337,7 @@ struct PagesCopyParams {
 };
 __global__ void __launch_bounds__(kCopyThreads)
 pages_copy_kernel(const PagesCopyParams p) {
+    cudaGridDependencySynchronize();                     // launched while the kernel that makes the list runs
     const int64_t step = static_cast<int64_t>(gridDim.x) * blockDim.x;
     if (p.table) {
         for (int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x; i < p.table_words; i += step) {
