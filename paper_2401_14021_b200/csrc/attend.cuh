@@ -478,7 +478,7 @@ attend_kernel(const AttendParams p) {
     constexpr int STAGES = attend_stages(NT, D);
     constexpr int STAGE = attend_stage_bytes(D);
     constexpr bool QREG = attend_q_in_regs(NT);
-    constexpr int TILES = NT == 1 ? 2 : 1;   // tiles that are worked on side by side
+    constexpr int TILES = NT == 1 || NT == 3 ? 2 : 1;   // tiles that are worked on side by side, where registers allow it
     extern __shared__ __align__(128) unsigned char attend_smem[];
     __shared__ __align__(8) int scratch[64];
     __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
