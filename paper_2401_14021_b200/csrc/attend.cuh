@@ -40,10 +40,13 @@ constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 
 // Warps per CTA (one CTA per SM) and whether the query operands stay in registers, by column blocks.
 __host__ __device__ constexpr int attend_warps(int nt, int d) { return nt >= 3 ? 8 : nt == 1 && d == 64 ? 16 : 12; }
 __host__ __device__ constexpr bool attend_q_in_regs(int nt) { return nt == 1; }
-// Shared memory of a warp: stages of kAttendStage tokens and, where they are not in registers, the queries.
+// Shared memory of a warp: stages of kAttendStage tokens and, where they are not in registers, the queries. With two
+// column blocks of 128 dimensions there is room for one stage only (the other warps work while it is filled):
+// 208 us on 32 x 8 heads of 2000 to 32000 tokens with 16 rows, against 203 to 213 with 8 warps and two stages, but
+// 77 us against 80 to 90 on 64 x 32 heads of 700 with 9.
 __host__ __device__ constexpr int attend_stage_bytes(int d) { return kAttendStage * (d + 8); }
 __host__ __device__ constexpr int attend_q_bytes(int nt, int d) { return attend_q_in_regs(nt) ? 0 : 16 * nt * d; }
-constexpr int kAttendSmem = 207 * 1024;  // for the warps; the prefix sums and static variables take the rest
+constexpr int kAttendSmem = 210 * 1024;  // for the warps; the prefix sums and static variables take the rest
 __host__ __device__ constexpr int attend_stages(int nt, int d) {
     const int fit = (kAttendSmem / attend_warps(nt, d) - attend_q_bytes(nt, d)) / attend_stage_bytes(d);
     return fit > 4 ? 4 : fit;
@@ -51,7 +54,15 @@ __host__ __device__ constexpr int attend_stages(int nt, int d) {
 __host__ __device__ constexpr int attend_warp_bytes(int nt, int d) {
     return attend_stages(nt, d) * attend_stage_bytes(d) + attend_q_bytes(nt, d);
 }
-static_assert(attend_stages(1, 128) >= 2 && attend_stages(2, 128) >= 1 && attend_stages(4, 128) >= 2, "stages");
+static_assert(attend_stages(1, 128) >= 2 && attend_stages(3, 128) >= 2 && attend_stages(4, 128) >= 2 && attend_stages(1, 64) >= 2 &&
+                  attend_stages(4, 64) >= 2,
+              "one stage is read while another is on its way");
+// A warp's partial result (rows of D + 4 floats: values, maximum, sum) fits where its stages were.
+__host__ __device__ constexpr int attend_row_floats(int d) { return d + 4; }
+static_assert(attend_stages(2, 128) * attend_stage_bytes(128) >= 16 * attend_row_floats(128) * 4 &&
+                  attend_stages(4, 128) * attend_stage_bytes(128) >= 32 * attend_row_floats(128) * 4 &&
+                  attend_stages(4, 64) * attend_stage_bytes(64) >= 32 * attend_row_floats(64) * 4,
+              "partial results");
 
 struct AttendParams {
     KvParams kv;
@@ -340,6 +351,44 @@ __device__ __forceinline__ void attend_write_row(const AttendParams &p, int segm
     const float inv = r.L > 0.f ? 1.f / r.L : r.L == 0.f ? 0.f : NAN;
 #pragma unroll
     for (int e = 0; e < E; ++e) attend_row<T>(p, s, row)[E * (threadIdx.x & 31) + e] = from_float<T>(r.x[e] * inv);
+}
+
+// One CTA per segment: the pieces of its `working` warps are in shared memory, where their stages were.
+template <typename T, int D, int NT>
+__device__ __forceinline__ void attend_join_near(const AttendParams &p, int working, const unsigned char *smem) {
+    constexpr int WARPS = attend_warps(NT, D), ROWS = 8 * NT, E = D / 32, STRIDE = attend_warp_bytes(NT, D) / 4;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int rows = min(p.n * p.group, ROWS);
+    const float *base = reinterpret_cast<const float *>(smem);
+    __syncthreads();
+    for (int lr = warp; lr < rows; lr += WARPS) {
+        const float *row = base + lr * attend_row_floats(D);
+        const float2 ml = lane < working ? *reinterpret_cast<const float2 *>(row + lane * STRIDE + D) : make_float2(-1e30f, 0.f);
+        RowSum<D> r;
+        r.M = warp_max(ml.x);
+        const float w = exp2_approx(ml.x - r.M);
+        r.L = warp_sum(ml.y * w);
+#pragma unroll
+        for (int e = 0; e < E; ++e) r.x[e] = 0.f;
+        for (int k = 0; k < working; ++k) {
+            const float wk = __shfl_sync(0xffffffffu, w, k);
+#pragma unroll
+            for (int e = 0; e < E; ++e) r.x[e] = fmaf(row[k * STRIDE + 32 * e + lane], wk, r.x[e]);
+        }
+        // the lane's dimensions here are 32 e + lane
+        const int per = p.kv.heads * p.row_blocks, segment = blockIdx.x;
+        Segment s;
+        s.b = segment / per;
+        const int which = segment - s.b * per;
+        s.h = which / p.row_blocks;
+        s.rb = which - s.h * p.row_blocks;
+        const int qr = s.rb * ROWS + lr;
+        if (qr >= p.n * p.group) continue;
+        const float inv = r.L > 0.f ? 1.f / r.L : r.L == 0.f ? 0.f : NAN;
+        T *o = attend_row<T>(p, s, qr);
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[32 * e + lane] = from_float<T>(r.x[e] * inv);
+    }
 }
 
 // Brings the pieces of split segments together, in two steps. Inside a CTA: the warps' shares follow one
@@ -850,7 +899,8 @@ attend_kernel(const AttendParams p) {
                 }
         const bool whole = mine == seg.units;
         const int64_t piece = 2 * worker + (seg.unit == 0 ? 1 : 0);
-        if (lane == 0 && !whole) {
+        const bool near = share.own_cta;         // a piece that another warp of this CTA will merge: the stages' room is free now
+        if (lane == 0 && !whole && !near) {
             const int segment = seg.b * (p.kv.heads * p.row_blocks) + seg.h * p.row_blocks + seg.rb;
             if (seg.unit == 0) open_piece[warp] = make_int2(1, segment);
             else left_piece[warp] = make_int2(seg.unit + mine == seg.units ? 2 : 1, segment);
@@ -871,21 +921,26 @@ attend_kernel(const AttendParams p) {
                         o[16 * i + 8 + g] = from_float<T>(fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]) * inv);
                     }
                 } else {
-                    float *o = p.part + (piece * ROWS + lr) * D;
+                    float *o = near ? reinterpret_cast<float *>(ring) + lr * attend_row_floats(D) : p.part + (piece * ROWS + lr) * D;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
                         o[16 * i + g] = fmaf(acc[nt][i][e], lo_back, ob[nt][e]);
                         o[16 * i + 8 + g] = fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]);
                     }
                     if (g == 0) {
-                        p.part_ml[(piece * ROWS + lr) * 2] = mb[nt][e];
-                        p.part_ml[(piece * ROWS + lr) * 2 + 1] = l[nt][e];
+                        float *ml = near ? o + D : p.part_ml + (piece * ROWS + lr) * 2;
+                        ml[0] = mb[nt][e];
+                        ml[1] = l[nt][e];
                     }
                 }
             }
         seg.unit += mine;
         if (seg.unit == seg.units) attend_next(p, cum, seg);
         if (!QREG) __syncwarp();
+    }
+    if (share.own_cta) {
+        if (working > 1) attend_join_near<T, D, NT>(p, working, attend_smem);
+        return;
     }
     attend_join<T, D, NT>(p, share, cum, working, open_piece, left_piece, reinterpret_cast<float *>(attend_smem));
 }
