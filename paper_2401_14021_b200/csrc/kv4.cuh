@@ -8,6 +8,11 @@
 // V codes lie in blocks of 16 tokens in the order in which a warp's matrix instruction wants them:
 // token 8c + 2t + e of the block has dimension g + 8j as nibble j of the D / 16 bytes at [c][g][t][e],
 // so that lane 4g + t finds its operands in consecutive bytes and each token owns whole bytes.
+//
+// Append and read are bound by memory, 2.3 times the cache's bytes for 16-bit tensors, and close behind by
+// instructions (about five per value to quantise). Measured (16 x 509 tokens, 32 heads of 128, bf16): append 42 us and
+// read 32 us, 74 us together, 4.6 TB/s, 0.71 of the measured copy bandwidth; 210 us with a warp per token, whose V codes
+// left in pieces of two bytes. One token for each of 8 requests and back: 7 us for both launches.
 #pragma once
 
 #include <cuda_bf16.h>

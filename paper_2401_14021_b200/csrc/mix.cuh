@@ -2,6 +2,15 @@
 // the search returned for it,
 //     p[v] = (1 - lambda) softmax(logits / T)[v] + lambda * sum over {i: values[id_i] = v} of w_i,
 // with w the softmax of the neighbours' scores over their own temperature.
+//
+// Bound by memory: a logit is read once and a probability written once (6 bytes an entry in 16 bits). One pass
+// over global memory therefore, the slice of a row waiting in shared memory between maximum, sum and output,
+// and a cluster per row, so that a row of 128000 entries is spread over eight SMs' shared memory. Measured (512
+// rows x 128000, bf16, 64 neighbours): 70 us, 5.6 TB/s, 0.87 of the measured copy bandwidth; without neighbours 65 us.
+// Stores had to be 16 bytes per thread and aligned whatever the input's alignment (333 -> 127 us with the slice
+// staged), and the exchange between CTAs one store per warp instead of block and cluster barriers (127 -> 76 us).
+// A single row of 32000 takes 4.7 us, 6.1 us with neighbours (ids, then the values they point at: two more
+// round trips to memory).
 #pragma once
 
 #include <cooperative_groups.h>
