@@ -336,13 +336,13 @@ typedef enum { RALM_F16 = 0, RALM_BF16 = 1, RALM_F32 = 2 } ralm_dtype_t;
  *   ids, scores  [R][k] as ralm_search wrote them, 0 <= k <= RALM_MAX_K. An id outside [0, N), a value
  *           outside [0, V) and a score that is not finite are left out (padding of a short list).
  *   values  int32 [N], the token that follows each datastore entry.
- *   probs   fp32 [R][V], row pitch ld_probs (written).
+ *   probs   fp32 [R][V], row pitch ld_probs (written); must not overlap the logits.
  * A row with no neighbour left is softmax(logits / temperature) alone (k == 0 asks for just that), a
  * row whose logits are all -inf is the neighbours' distribution alone, a row with neither is zeros. A
  * NaN or +inf among the logits makes the row NaN, as in a softmax. Neighbours' weights are added in
  * fixed point: the result does not depend on the order of the atomics.
  * Errors: INVALID_ARG (null pointers, sizes, pitch < V, lambda outside [0, 1], temperatures not
- * positive and finite, dtype or metric unknown). R == 0 is a no-op. */
+ * positive and finite, dtype or metric unknown, logits == probs). R == 0 is a no-op. */
 ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_logits, int32_t R, int32_t V,
                            const int64_t *ids, const float *scores, int32_t k, ralm_metric_t metric,
                            const int32_t *values, int64_t N, float lambda, float temperature,
@@ -448,7 +448,7 @@ typedef struct {
 
 /* Quantise the tokens into positions starts .. starts + count - 1, which lie below the row's length
  * (ralm_pages_resize first) in pages that no other row holds. Others are left out, and the status word
- * says RALM_ERR_INVALID_ARG. */
+ * says RALM_ERR_INVALID_ARG. No position may be written by two entries of one call. */
 ralm_status_t ralm_kv_append(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream);
 
 /* The values that positions starts .. starts + n - 1 stand for; zeros at positions outside the row or
@@ -459,7 +459,8 @@ ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_
  * q_len is NULL) stands at position length - m + i and sees the keys up to and including it. One token per
  * entry is a decode step, drafts + 1 of them a verification. Queries that see nothing, and those at
  * or beyond q_len, give zeros.
- *   q, out   [batch][n][q_heads][head_dim], fp16 or bf16, strides in elements, last dimension contiguous;
+ *   q, out   [batch][n][q_heads][head_dim], fp16 or bf16, strides in elements, last dimension contiguous; they
+ *            must not overlap (q == out is refused);
  *            q_heads a multiple of kv_heads, query head h reads key-value head h / (q_heads / kv_heads).
  *   workspace of ralm_kv_attend_workspace(...) bytes, 16-byte aligned, ZEROED by the caller before its first
  *            use; calls of any sizes may follow one another in it, one at a time. */

@@ -254,27 +254,29 @@ PyObject *verify_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// pages (address of a ralm_pages_t), new_lengths, stream
+// pages (address of a ralm_pages_t), its table (for the device), new_lengths, stream
 PyObject *pages_resize(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 3, [&]() -> PyObject * {
+    return guarded(n, 4, [&]() -> PyObject * {
         const auto *p = static_cast<const ralm_pages_t *>(pointer(a[0]));
         Args args;
-        const int32_t *to = args.dense<int32_t>(a[1], {p->rows}, at::kInt, "new_lengths");
-        Where w(args, a[2]);
+        args.tensor(a[1], "table");
+        const int32_t *to = args.dense<int32_t>(a[2], {p->rows}, at::kInt, "new_lengths");
+        Where w(args, a[3]);
         if (failed(calls.ralm_pages_resize(p, to, w.stream), "ralm_pages_resize")) return nullptr;
         Py_RETURN_NONE;
     });
 }
 
-// pages, src, dst, stream
+// pages, table, src, dst, stream
 PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 4, [&]() -> PyObject * {
+    return guarded(n, 5, [&]() -> PyObject * {
         const auto *p = static_cast<const ralm_pages_t *>(pointer(a[0]));
         Args args;
-        const int64_t count = args.tensor(a[1], "src")->numel();
-        const int32_t *src = args.dense<int32_t>(a[1], {count}, at::kInt, "src");
-        const int32_t *dst = args.dense<int32_t>(a[2], {count}, at::kInt, "dst");
-        Where w(args, a[3]);
+        args.tensor(a[1], "table");
+        const int64_t count = args.tensor(a[2], "src")->numel();
+        const int32_t *src = args.dense<int32_t>(a[2], {count}, at::kInt, "src");
+        const int32_t *dst = args.dense<int32_t>(a[3], {count}, at::kInt, "dst");
+        Where w(args, a[4]);
         if (failed(calls.ralm_pages_fork(p, src, dst, size32(count, "n"), w.stream), "ralm_pages_fork")) return nullptr;
         Py_RETURN_NONE;
     });
@@ -292,16 +294,18 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// source pages, from, destination pages, to, stream
+// source pages, from, destination pages, to, destination table, source table, stream
 PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 5, [&]() -> PyObject * {
+    return guarded(n, 7, [&]() -> PyObject * {
         const auto *s = static_cast<const ralm_pages_t *>(pointer(a[0]));
         const auto *d = static_cast<const ralm_pages_t *>(pointer(a[2]));
         Args args;
+        args.tensor(a[4], "table");
+        args.tensor(a[5], "the source's table");
         const int64_t count = args.tensor(a[1], "src")->numel();
         const int32_t *from = args.dense<int32_t>(a[1], {count}, at::kInt, "src");
         const int32_t *to = args.dense<int32_t>(a[3], {count}, at::kInt, "dst");
-        Where w(args, a[4]);
+        Where w(args, a[6]);
         if (failed(calls.ralm_pages_copy(s, from, d, to, size32(count, "n"), w.stream), "ralm_pages_copy")) return nullptr;
         Py_RETURN_NONE;
     });
@@ -330,11 +334,12 @@ ralm_kv_tokens_t kv_tokens(Args &args, const ralm_kv_t *c, PyObject *ko, PyObjec
     return t;
 }
 
-// cache (address of a ralm_kv_t), layer, k, v, starts, count, rows, stream
+// cache (address of a ralm_kv_t), layer, k, v, starts, count, rows, stream, table
 PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 8, [&]() -> PyObject * {
+    return guarded(n, 9, [&]() -> PyObject * {
         const auto *c = static_cast<const ralm_kv_t *>(pointer(a[0]));
         Args args;
+        args.tensor(a[8], "table");
         const ralm_kv_tokens_t t = kv_tokens(args, c, a[2], a[3], a[4], a[5], a[6]);
         Where w(args, a[7]);
         if (failed(calls.ralm_kv_append(c, int32(a[1], "layer"), &t, w.stream), "ralm_kv_append")) return nullptr;
@@ -342,9 +347,10 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 8, [&]() -> PyObject * {
+    return guarded(n, 9, [&]() -> PyObject * {
         const auto *c = static_cast<const ralm_kv_t *>(pointer(a[0]));
         Args args;
+        args.tensor(a[8], "table");
         const ralm_kv_tokens_t t = kv_tokens(args, c, a[2], a[3], a[4], a[5], a[6]);
         Where w(args, a[7]);
         if (failed(calls.ralm_kv_read(c, int32(a[1], "layer"), &t, w.stream), "ralm_kv_read")) return nullptr;

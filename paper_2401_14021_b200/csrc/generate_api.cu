@@ -243,7 +243,7 @@ ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_lo
         std::isinf(knn_temperature))
         return RALM_ERR_INVALID_ARG;
     if (R == 0) return RALM_OK;
-    if (!logits || !probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
+    if (!logits || !probs || logits == probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
     if (reinterpret_cast<uintptr_t>(logits) % (dtype == RALM_F32 ? 4 : 2) != 0) return RALM_ERR_INVALID_ARG;
     if (static_cast<int64_t>(R) * kMixMaxCluster >= (int64_t{1} << 31)) return RALM_ERR_INVALID_ARG;
     const int sms = sm_count();
@@ -394,7 +394,7 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
         return RALM_ERR_INVALID_ARG;
     if (cache->head_dim != 64 && cache->head_dim != 128) return RALM_ERR_UNSUPPORTED;
     if (a->batch == 0 || a->n == 0) return RALM_OK;
-    if (!a->q || !a->out || !a->workspace || !aligned16(a->workspace)) return RALM_ERR_INVALID_ARG;
+    if (!a->q || !a->out || a->q == a->out || !a->workspace || !aligned16(a->workspace)) return RALM_ERR_INVALID_ARG;
     const int group = a->q_heads / cache->kv_heads;
     const int64_t rows = static_cast<int64_t>(group) * a->n;
     const ralm_pages_t &pg = cache->pages;

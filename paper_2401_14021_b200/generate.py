@@ -85,6 +85,8 @@ class Pages:
         rows, max_pages = table.shape
         pages = refs.shape[0]
         _shape(lengths, (rows,), "lengths")
+        if any(t is not None and t.device != table.device for t in (pool, lengths, refs)):
+            raise TypeError("pool, table, lengths and refs must be on one device")
         self.pool, self.table, self.lengths, self.refs, self.page_size = pool, table, lengths, refs, page_size
         c = _Pages(pages=pages, rows=rows, max_pages=max_pages, page_size=page_size)
         c.table, c.lengths, c.refs = (_dev(t, torch.int32, n) for t, n in
@@ -114,11 +116,11 @@ class Pages:
 
     def resize(self, new_lengths: torch.Tensor, stream=None):
         """ralm_pages_resize: give back, copy on write and take pages for new_lengths int32 [rows]."""
-        self._call.pages_resize(self._ptr, new_lengths, stream)
+        self._call.pages_resize(self._ptr, self.table, new_lengths, stream)
 
     def fork(self, src: torch.Tensor, dst: torch.Tensor, stream=None):
         """ralm_pages_fork: rows dst int32 [n] come to hold the pages of rows src int32 [n]."""
-        self._call.pages_fork(self._ptr, src, dst, stream)
+        self._call.pages_fork(self._ptr, self.table, src, dst, stream)
 
     def compact(self, stream=None) -> torch.Tensor:
         """ralm_pages_compact: live pages become 0 .. live - 1; returns live, int32 [1] on the device."""
@@ -126,7 +128,7 @@ class Pages:
 
     def copy_from(self, other: "Pages", src: torch.Tensor, dst: torch.Tensor, stream=None):
         """ralm_pages_copy: contents of `other`'s pages src int32 [n] into this pool's pages dst int32 [n]."""
-        self._call.pages_copy(other._ptr, src, self._ptr, dst, stream)
+        self._call.pages_copy(other._ptr, src, self._ptr, dst, self.table, other.table, stream)
 
     def device_status(self, stream=None) -> int:
         """ralm_pages_status: reads and clears the status word (synchronises)."""
@@ -171,7 +173,7 @@ class KVCache(Pages):
                rows: torch.Tensor = None, stream=None):
         """ralm_kv_append: k, v [batch][n][kv_heads][head_dim] (fp16 or bf16) into positions starts
         int32 [batch] and on, below the rows' lengths."""
-        self._call.kv_append(self._kv_ptr, layer, k, v, starts, count, rows, stream)
+        self._call.kv_append(self._kv_ptr, layer, k, v, starts, count, rows, stream, self.table)
 
     def read(self, layer: int, starts: torch.Tensor, n: int, dtype=torch.float16, k: torch.Tensor = None,
              v: torch.Tensor = None, count: torch.Tensor = None, rows: torch.Tensor = None, stream=None):
@@ -182,7 +184,7 @@ class KVCache(Pages):
             v = torch.empty(shape, dtype=k.dtype, device=starts.device) if v is None else v
         if k.dim() != 4 or k.shape[1] != n:
             raise TypeError("k must be [batch][%d][kv_heads][head_dim]" % n)
-        return self._call.kv_read(self._kv_ptr, layer, k, v, starts, count, rows, stream)
+        return self._call.kv_read(self._kv_ptr, layer, k, v, starts, count, rows, stream, self.table)
 
     def attend(self, layer: int, q: torch.Tensor, scale: float = None, q_len: torch.Tensor = None,
                rows: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:

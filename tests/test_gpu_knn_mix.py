@@ -167,3 +167,6 @@ def test_refusals():
         ralm.knn_mix(logits[:1], big, big.float(), values, 0.5)                     # more neighbours than a search returns
     with pytest.raises(TypeError):
         ralm.knn_mix(logits, ids, scores, values, 0.5, probs=torch.empty((2, 100), dtype=torch.float16, device=DEV))
+    same = logits.float()
+    with pytest.raises(ralm.RalmError):
+        ralm.knn_mix(same, ids, scores, values, 0.5, probs=same)                   # in place

@@ -404,6 +404,8 @@ def test_refusals():
         with pytest.raises(ralm.RalmError) as e:
             cache.attend(layer, torch.randn((2, 1, heads, 64), device=DEV).half(), scale=scale)
         assert e.value.status == 1
+    with pytest.raises(ralm.RalmError):
+        cache.attend(0, q, out=q)                                                 # in place
     for args in ((x.float(), x.float()), (x, x.bfloat16()), (x[:, :, :1], x[:, :, :1]), (x, x[:1])):
         with pytest.raises(TypeError):
             cache.append(0, *args, i32([0, 0]))
