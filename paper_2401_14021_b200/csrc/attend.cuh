@@ -308,27 +308,26 @@ __device__ __forceinline__ T *attend_row(const AttendParams &p, const Segment &s
 template <int D> struct RowSum {
     float x[D / 32], M, L;
 };
-// Merges pieces first, first + stride, .. (`count` of them, the first possibly elsewhere) of one query row; a warp.
-// A piece is a row of D values and a (maximum, sum). `share`: this warp takes every `parts`-th piece, from `part` on.
+// Merges `count` pieces of one query row; a warp. A piece is a row of D values and a (maximum, sum), which the lanes
+// keep for the first 32 pieces. This warp takes every `parts`-th piece, from `part` on; M is of all of them.
 template <int D, typename Piece>
 __device__ __forceinline__ RowSum<D> attend_merge(int count, int part, int parts, Piece piece_of, const float *values, const float *ml) {
     constexpr int E = D / 32;
     const int lane = threadIdx.x & 31;
+    auto pair = [&](int j) { return j < count ? __ldcg(reinterpret_cast<const float2 *>(ml + 2 * piece_of(j))) : make_float2(-1e30f, 0.f); };
     RowSum<D> r;
-    r.M = -1e30f;
-    for (int j = lane; j < count; j += 32) r.M = fmaxf(r.M, __ldcg(ml + 2 * piece_of(j)));
+    const float2 mine = pair(part + lane * parts);
+    r.M = mine.x;
+    if (parts > 1 || count > 32)
+        for (int j = lane; j < count; j += 32) r.M = fmaxf(r.M, pair(j).x);
     r.M = warp_max(r.M);
     r.L = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) r.x[e] = 0.f;
     for (int j0 = part; j0 < count; j0 += 32 * parts) {
-        const int j = j0 + lane * parts;
-        float w = 0.f;
-        if (j < count) {
-            const float2 p = __ldcg(reinterpret_cast<const float2 *>(ml + 2 * piece_of(j)));
-            w = exp2_approx(p.x - r.M);
-            r.L = fmaf(p.y, w, r.L);
-        }
+        const float2 p = j0 == part ? mine : pair(j0 + lane * parts);
+        const float w = exp2_approx(p.x - r.M);                     // 0 where there is no piece
+        r.L = fmaf(p.y, w, r.L);
         const int some = min(32, (count - j0 + parts - 1) / parts);
 #pragma unroll 4
         for (int i = 0; i < some; ++i) {
@@ -456,25 +455,34 @@ __device__ __forceinline__ void attend_join(const AttendParams &p, const Share &
     // the CTA's own pieces: of the segment that came in, and of the one that goes out (which may be the same)
     const int last_leader = 31 - __clz(opens);
     last_open = opens != 0 && (last_leader + 1 >= 32 || (ends >> (last_leader + 1)) == 0);
-    __shared__ int merge_from;
-    for (int turn = 0; turn < 2; ++turn) {
-        const bool mine = turn == 0 ? carried : last_open;
-        if (!mine) continue;                                            // the same for the whole CTA
-        const int segment = turn == 0 ? left_piece[0].y : open_piece[last_leader].y;
-        const int per = p.kv.heads * p.row_blocks;
-        const int b = segment / per, units = cum[b + 1] - cum[b];
-        const long long first = static_cast<long long>(cum[b]) * per + static_cast<long long>(segment - b * per) * units;
-        const int c0 = share.owner(first) / WARPS, c1 = share.owner(first + units - 1) / WARPS;
-        __syncthreads();
-        if (threadIdx.x == 0) {
-            __threadfence();
-            const int before = atomicAdd(&p.counters[c0], 1);
-            merge_from = before == c1 - c0 ? c0 : -1;
-            if (merge_from >= 0) p.counters[c0] = 0;
-            __threadfence();
+    __shared__ int merge[2], merge_from[2], merge_to[2];
+    if (threadIdx.x < 2) merge[threadIdx.x] = 0;
+    __syncthreads();
+    // one thread each counts this CTA in at the first CTA of the segment that came in, and of the one that goes out
+    if (threadIdx.x % 32 == 0 && threadIdx.x < 64) {
+        const int turn = threadIdx.x / 32;
+        if (turn == 0 ? carried : last_open) {
+            const int segment = turn == 0 ? left_piece[0].y : open_piece[last_leader].y;
+            const int per = p.kv.heads * p.row_blocks;
+            const int b = segment / per, units = cum[b + 1] - cum[b];
+            const long long first = static_cast<long long>(cum[b]) * per + static_cast<long long>(segment - b * per) * units;
+            const int c0 = share.owner(first) / WARPS, c1 = share.owner(first + units - 1) / WARPS;
+            // releases this CTA's pieces (the barrier above is before it) and acquires the others'
+            int before;
+            asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(p.counters + c0) : "memory");
+            if (before == c1 - c0) {
+                p.counters[c0] = 0;
+                merge[turn] = 1;
+                merge_from[turn] = c0;
+                merge_to[turn] = c1;
+            }
         }
-        __syncthreads();
-        if (merge_from < 0) continue;
+    }
+    __syncthreads();
+    for (int turn = 0; turn < 2; ++turn) {
+        if (!merge[turn]) continue;                                     // the same for the whole CTA
+        const int segment = turn == 0 ? left_piece[0].y : open_piece[last_leader].y;
+        const int c0 = merge_from[turn], c1 = merge_to[turn];
         // few rows: several warps share a row, every parts-th piece each
         const int count = c1 - c0 + 1, parts = max(WARPS / rows, 1);
         for (int i0 = 0; i0 < rows * parts; i0 += WARPS) {
