@@ -76,6 +76,9 @@ ralm_status_t launch_cluster(void (*kernel)(Params), int rows, int cluster, int 
 // A row is cut over a cluster so that a slice is about 32 KB (six CTAs then fit an SM, and one CTA's
 // stores overlap another's loads), and further while there are fewer CTAs than the GPU can hold; but not
 // below one vector per thread.
+// The neighbours' table has twice as many slots as neighbours, up to 16 KB: half full at most it is quicker where
+// one CTA per SM waits for it (1 row x 32000, 64 neighbours: 5.8 us, 6.4 with as many slots as neighbours), but
+// 32 KB would leave room for fewer CTAs (72 rows x 50257, 1024 neighbours: 17.2 us, 16.0 with 16 KB).
 constexpr int kMixSlice = 32 * 1024;
 constexpr int kMixMaxStage = 160 * 1024;   // bytes of a slice that a CTA keeps in shared memory
 
@@ -89,10 +92,10 @@ ralm_status_t launch_mix(MixParams p, int R, int sms, cudaStream_t st) {
         cluster *= 2;
     p.slice = static_cast<int>(slice_of(cluster));
     p.slots = 1;
-    while (p.slots < 2 * p.k) p.slots *= 2;
+    while (p.slots < std::min(2 * p.k, RALM_MAX_K)) p.slots *= 2;
     const size_t hash = p.k > 0 ? p.slots * 16 : 0, bytes = p.slice * sizeof(T);
     if (bytes > kMixMaxStage) return launch_cluster(mix_kernel<T, false>, R, cluster, kMixThreads, hash, st, p);
-    if (!allow_smem<mix_kernel<T, true>>(kMixMaxStage + 32 * RALM_MAX_K)) return RALM_ERR_CUDA;
+    if (!allow_smem<mix_kernel<T, true>>(kMixMaxStage + 16 * RALM_MAX_K)) return RALM_ERR_CUDA;
     return launch_cluster(mix_kernel<T, true>, R, cluster, kMixThreads, bytes + hash, st, p);
 }
 

@@ -56,7 +56,7 @@ struct MixParams {
     float *probs;
     int64_t ld_probs;
     int slice;           // elements of a row that one CTA of the cluster handles, a multiple of 16
-    int slots;           // hash slots for the neighbours' tokens, a power of two, at least 2 k
+    int slots;           // hash slots for the neighbours' tokens, a power of two, at least k
 };
 
 template <typename T> struct MixVec {
@@ -277,7 +277,7 @@ mix_kernel(const MixParams p) {
             const int pos = token[j] - base;
             if (pos < 0 || pos >= p.slice) continue;
             int h = (token[j] * 0x9E3779B1u) >> 20 & (p.slots - 1);
-            for (;;) {                                // at most k tokens in 2 k slots: there is always a free one
+            for (;;) {                                // at most k tokens in k slots or more: there is always a place
                 const uint32_t seen = atomicCAS(&slots[h].w, 0xFFFFFFFFu, static_cast<uint32_t>(token[j]));
                 if (seen == 0xFFFFFFFFu) own[j] = h;
                 if (seen == 0xFFFFFFFFu || seen == static_cast<uint32_t>(token[j])) break;
