@@ -559,6 +559,7 @@ attend_kernel(const AttendParams p) {
         for (int i = 0; i < STAGES; ++i) mbar_init(bar0 + 8 * i, 1);
         mbar_fence_init();
     }
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     const Share share = attend_share(p, cum, scratch);
     const int worker = blockIdx.x * WARPS + warp;
     Segment mine_first;                  // where the warp begins, and how many units it takes

@@ -34,8 +34,6 @@ int sm_count() {
     return n;
 }
 
-ralm_status_t launched() { return cudaGetLastError() == cudaSuccess ? RALM_OK : RALM_ERR_CUDA; }
-
 // Lets a kernel use up to `most` bytes of dynamic shared memory; asked once per kernel and device.
 template <auto Kernel>
 bool allow_smem(int most) {
@@ -67,6 +65,27 @@ ralm_status_t launch_cluster(void (*kernel)(Params), int rows, int cluster, int 
     cfg.attrs = attr;
     cfg.numAttrs = 1;
     if (cudaLaunchKernelEx(&cfg, kernel, params) != cudaSuccess) {
+        cudaGetLastError();
+        return RALM_ERR_CUDA;
+    }
+    return RALM_OK;
+}
+
+// The kernel may be set up while the last blocks of the one before it in the stream run out; it waits for that
+// one's end (with all that it wrote) before it reads anything.
+template <typename... P, typename... A>
+ralm_status_t launch(void (*kernel)(P...), int64_t blocks, int threads, size_t smem, cudaStream_t st, const A &...args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+    cfg.blockDim = dim3(threads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, kernel, P(args)...) != cudaSuccess) {
         cudaGetLastError();
         return RALM_ERR_CUDA;
     }
@@ -114,20 +133,7 @@ ralm_status_t launch_copy(const PagesCopyParams &p, int64_t most, cudaStream_t s
     if (sms == 0) return RALM_ERR_CUDA;
     const int64_t jobs = most * std::max(p.layers, 1) * ((p.page_bytes + 16383) / 16384);
     const int64_t blocks = std::max<int64_t>(1, std::min<int64_t>(jobs, 8LL * sms));
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(static_cast<unsigned>(blocks));
-    cfg.blockDim = dim3(kCopyThreads);
-    cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, pages_copy_kernel, p) != cudaSuccess) {
-        cudaGetLastError();
-        return RALM_ERR_CUDA;
-    }
-    return RALM_OK;
+    return launch(pages_copy_kernel, blocks, kCopyThreads, 0, st, p);
 }
 PagesCopyParams copy_in_pool(const ralm_pages_t &p) {
     PagesCopyParams c = {};
@@ -174,9 +180,7 @@ ralm_status_t launch_tokens(bool append, const KvParams &k, const KvTokens &t, i
     const int64_t jobs = static_cast<int64_t>(k.batch) * kv_blocks(t.n) * k.heads;
     if (jobs >= (int64_t{1} << 31)) return RALM_ERR_UNSUPPORTED;
     const int blocks = static_cast<int>(std::min<int64_t>((jobs + kKvThreads / 32 - 1) / (kKvThreads / 32), 32LL * sms));
-    if (append) kv_append_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
-    else kv_read_kernel<T, D><<<blocks, kKvThreads, 0, st>>>(k, t);
-    return launched();
+    return launch(append ? kv_append_kernel<T, D> : kv_read_kernel<T, D>, blocks, kKvThreads, 0, st, k, t);
 }
 ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ralm_kv_tokens_t *t, void *stream) {
     if (!kv_ok(c, layer) || !t || t->batch < 0 || t->n < 0 || (t->dtype != RALM_F16 && t->dtype != RALM_BF16))
@@ -217,8 +221,7 @@ ralm_status_t launch_attend(AttendParams p, int sms, cudaStream_t st) {
     p.cta_ml = p.part_ml + static_cast<int64_t>(2) * p.workers * 8 * NT * 2;
     p.part = p.cta_ml + static_cast<int64_t>(2) * attend_counters(sms) * 8 * NT * 2;
     p.cta_part = p.part + static_cast<int64_t>(2) * p.workers * 8 * NT * D;
-    attend_kernel<T, D, NT><<<sms, kThreads, kRing + cum, st>>>(p);
-    return launched();
+    return launch(attend_kernel<T, D, NT>, sms, kThreads, kRing + cum, st, p);
 }
 template <typename T, int D>
 ralm_status_t launch_attend(const AttendParams &p, int nt, int sms, cudaStream_t st) {
@@ -312,8 +315,7 @@ ralm_status_t ralm_pages_resize(const ralm_pages_t *pages, const int32_t *new_le
     if (pages->rows == 0) return RALM_OK;
     if (!new_lengths) return RALM_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    pages_resize_kernel<<<1, kPagesThreads, 0, st>>>(*pages, new_lengths);
-    ralm_status_t rs = launched();
+    const ralm_status_t rs = launch(pages_resize_kernel, 1, kPagesThreads, 0, st, *pages, new_lengths);
     if (rs != RALM_OK || !pages->pool) return rs;
     return launch_copy(copy_in_pool(*pages), std::min(pages->rows, pages->pages), st);   // at most one page per row
 }
@@ -322,15 +324,14 @@ ralm_status_t ralm_pages_fork(const ralm_pages_t *pages, const int32_t *src, con
     if (!pages_ok(pages) || n < 0 || n > pages->rows) return RALM_ERR_INVALID_ARG;
     if (n == 0) return RALM_OK;
     if (!src || !dst) return RALM_ERR_INVALID_ARG;
-    pages_fork_kernel<<<1, kPagesThreads, (pages->rows + 31) / 32 * sizeof(int), static_cast<cudaStream_t>(stream)>>>(*pages, src, dst, n);
-    return launched();
+    return launch(pages_fork_kernel, 1, kPagesThreads, (pages->rows + 31) / 32 * sizeof(int), static_cast<cudaStream_t>(stream), *pages,
+                  src, dst, n);
 }
 
 ralm_status_t ralm_pages_compact(const ralm_pages_t *pages, int32_t *live, void *stream) {
     if (!pages_ok(pages) || (pages->pool && !pool_ok(pages)) || !live) return RALM_ERR_INVALID_ARG;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    pages_compact_kernel<<<1, kPagesThreads, 0, st>>>(*pages, live);
-    ralm_status_t rs = launched();
+    const ralm_status_t rs = launch(pages_compact_kernel, 1, kPagesThreads, 0, st, *pages, live);
     if (rs != RALM_OK) return rs;
     PagesCopyParams c = copy_in_pool(*pages);
     c.table = pages->table;

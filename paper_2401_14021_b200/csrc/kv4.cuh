@@ -273,6 +273,7 @@ __device__ __forceinline__ void kv_values(uint32_t word, __half2 pair, __nv_bflo
 template <typename T, int D>
 __global__ void __launch_bounds__(kKvThreads, 4)
 kv_append_kernel(const KvParams p, const KvTokens t) {
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     using Block = KvBlock<D>;
     const int lane = threadIdx.x & 31, part = lane % Block::kLanes;
     const int ps = p.page_size;
@@ -336,6 +337,7 @@ kv_append_kernel(const KvParams p, const KvTokens t) {
 template <typename T, int D>
 __global__ void __launch_bounds__(kKvThreads, 6)
 kv_read_kernel(const KvParams p, const KvTokens t) {
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     using Block = KvBlock<D>;
     const int lane = threadIdx.x & 31, part = lane % Block::kLanes;
     const int ps = p.page_size;

@@ -70,6 +70,7 @@ constexpr int kPagesSmemList = 4096;   // free pages that the resize kernel keep
 // the list that this kernel leaves in the workspace.
 __global__ void __launch_bounds__(kPagesThreads, 1)
 pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_lengths) {
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     __shared__ int buf[kPagesWarps];
     __shared__ int near_list[kPagesSmemList];
     __shared__ int flags;
@@ -227,6 +228,7 @@ pages_resize_kernel(const ralm_pages_t p, const int32_t *__restrict__ new_length
 // seen: one bit per row, dynamic shared memory.
 __global__ void __launch_bounds__(kPagesThreads, 1)
 pages_fork_kernel(const ralm_pages_t p, const int32_t *__restrict__ src, const int32_t *__restrict__ dst, int n) {
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     extern __shared__ unsigned int seen[];
     __shared__ int bad;
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -271,6 +273,7 @@ pages_fork_kernel(const ralm_pages_t p, const int32_t *__restrict__ src, const i
 // or above `live` goes to the i-th hole below it. One CTA. w.list[page]: the page's new number.
 __global__ void __launch_bounds__(kPagesThreads, 1)
 pages_compact_kernel(const ralm_pages_t p, int32_t *__restrict__ live_out) {
+    cudaGridDependencySynchronize();                     // what ran before in the stream has ended
     __shared__ int buf[kPagesWarps];
     const PagesWork w = pages_work(p);
     const int tid = threadIdx.x;
