@@ -11,7 +11,7 @@
 //
 // Append and read are bound by memory, 2.3 times the cache's bytes for 16-bit tensors, and close behind by
 // instructions (about five per value to quantise). Measured (16 x 509 tokens, 32 heads of 128, bf16): append 42 us and
-// read 32 us, 74 us together, 4.6 TB/s, 0.71 of the measured copy bandwidth; 210 us with a warp per token, whose V codes
+// read 32 us, 73 us together, 4.6 TB/s, 0.71 of the measured copy bandwidth; 210 us with a warp per token, whose V codes
 // left in pieces of two bytes. One token for each of 8 requests and back: 7 us for both launches.
 #pragma once
 
