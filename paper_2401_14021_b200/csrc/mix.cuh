@@ -55,7 +55,7 @@ struct MixParams {
     float lambda;
     float *probs;
     int64_t ld_probs;
-    int slice;           // elements of a row that one CTA of the cluster handles, a multiple of 16
+    int slice;           // elements of a row that one CTA of the cluster handles, a multiple of a 16-byte vector's 4 or 8
     int slots;           // hash slots for the neighbours' tokens, a power of two, at least k
 };
 
@@ -88,25 +88,31 @@ __device__ __forceinline__ float warp_sum(float v) {
 }
 // What the exponentials of a row are taken relative to. In powers of two the reference is a whole number r
 // at or above the largest exponent m scale: x scale - r is then one fused product and sum, rounded once, and
-// two references differ by an exact power of two. Where m scale is too large for that (rows whose logits are
-// all the type's lowest value, infinities) the differences x - m are scaled instead.
+// two references differ by an exact power of two. From 2^22 on the rounding of m scale itself would be a step of
+// more than 1/4, soon of more powers of two than 32 bits have (rows masked by -1e9 or lower throughout, small
+// temperatures): there the differences x - m are scaled instead.
+constexpr float kMixWide = 4194304.f;
 struct MixRef {
     float m, r;
     bool wide;
     __device__ __forceinline__ MixRef(float top, float scale) : m(top), r(0.f), wide(false) {
         if (top == -INFINITY) return;
         const float e = top * scale;
-        wide = !(fabsf(e) < 1e18f);
+        wide = !(fabsf(e) < kMixWide);
         if (!wide) r = ceilf(e);
     }
     __device__ __forceinline__ float power(float x, float scale) const {   // 2^(x scale) over the reference
         return wide ? exp2_approx((x - m) * scale) : exp2_approx(fmaf(x, scale, -r));
     }
 };
-// A sum relative to `from`, relative to `to`; one over nothing but -inf is 0 (or NaN) and stays as it is.
+// A sum relative to `from`, relative to `to`; one over nothing but -inf is 0 (or NaN) and stays as it is. A reference
+// is 2^(m scale) in the one form and 2^r in the other.
 __device__ __forceinline__ float rescaled(const MixRef &from, float s, const MixRef &to, float scale) {
     if (from.m == -INFINITY) return s;
-    return s * exp2_approx(from.wide || to.wide ? (from.m - to.m) * scale : from.r - to.r);
+    float e;
+    if (to.wide) e = from.wide ? (from.m - to.m) * scale : fmaf(-to.m, scale, from.r);
+    else e = from.wide ? fmaf(from.m, scale, -to.r) : from.r - to.r;
+    return s * exp2_approx(e);
 }
 __device__ __forceinline__ float vec_max(const MixVec<float> &u) { return fmaxf(fmaxf(u.x[0], u.x[1]), fmaxf(u.x[2], u.x[3])); }
 __device__ __forceinline__ float vec_max(const MixVec<__half> &u) {
