@@ -341,8 +341,9 @@ typedef enum { RALM_F16 = 0, RALM_BF16 = 1, RALM_F32 = 2 } ralm_dtype_t;
  * row whose logits are all -inf is the neighbours' distribution alone, a row with neither is zeros. A
  * NaN or +inf among the logits makes the row NaN, as in a softmax. Neighbours' weights are added in
  * fixed point: the result does not depend on the order of the atomics.
- * Errors: INVALID_ARG (null pointers, sizes, pitch < V, lambda outside [0, 1], temperatures not
- * positive and finite, dtype or metric unknown, logits == probs). R == 0 is a no-op. */
+ * Errors: INVALID_ARG (null pointers, sizes, pitch < V, lambda outside [0, 1], temperatures that are not
+ * positive and finite or below 4.3e-39, so that log2(e) over them is not finite, dtype or metric unknown,
+ * logits == probs). R == 0 is a no-op. */
 ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_logits, int32_t R, int32_t V,
                            const int64_t *ids, const float *scores, int32_t k, ralm_metric_t metric,
                            const int32_t *values, int64_t N, float lambda, float temperature,

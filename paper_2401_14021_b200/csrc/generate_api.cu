@@ -246,7 +246,7 @@ ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_lo
     if (dtype != RALM_F16 && dtype != RALM_BF16 && dtype != RALM_F32) return RALM_ERR_INVALID_ARG;
     if (metric != RALM_IP && metric != RALM_L2) return RALM_ERR_INVALID_ARG;
     if (!(lambda >= 0.f && lambda <= 1.f) || !(temperature > 0.f) || !(knn_temperature > 0.f) || std::isinf(temperature) ||
-        std::isinf(knn_temperature))
+        std::isinf(knn_temperature) || std::isinf(kLog2e / temperature) || std::isinf(kLog2e / knn_temperature))
         return RALM_ERR_INVALID_ARG;
     if (R == 0) return RALM_OK;
     if (!logits || !probs || logits == probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
@@ -263,7 +263,8 @@ ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_lo
     p.k = k;
     p.values = values;
     p.N = N;
-    p.score_scale = (metric == RALM_L2 ? -kLog2e : kLog2e) / knn_temperature;
+    p.score_sign = metric == RALM_L2 ? -1.f : 1.f;
+    p.score_scale = kLog2e / knn_temperature;
     p.logit_scale = kLog2e / temperature;
     p.lambda = lambda;
     p.probs = probs;

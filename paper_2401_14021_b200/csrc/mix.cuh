@@ -50,7 +50,8 @@ struct MixParams {
     int k;
     const int32_t *values;
     int64_t N;
-    float score_scale;   // log2(e) / knn temperature, negative for distances
+    float score_sign;    // -1 for distances
+    float score_scale;   // log2(e) / knn temperature
     float logit_scale;   // log2(e) / temperature
     float lambda;
     float *probs;
@@ -219,7 +220,7 @@ mix_kernel(const MixParams p) {
         for (int j = 0; j < kMixNeighbours; ++j) {
             const int i = tid + j * k_warps * 32;
             id[j] = i < p.k ? p.ids[static_cast<int64_t>(row) * p.k + i] : -1;
-            score[j] = i < p.k ? p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_scale : 0.f;
+            score[j] = i < p.k ? p.scores[static_cast<int64_t>(row) * p.k + i] * p.score_sign : 0.f;
         }
         for (int i = tid; i < p.slots; i += k_warps * 32) slots[i] = make_uint4(0, 0, 0, 0xFFFFFFFFu);
 #pragma unroll
@@ -278,7 +279,8 @@ mix_kernel(const MixParams p) {
         for (int j = 0; j < kMixNeighbours; ++j) {
             own[j] = in_slot[j] = -1;
             if (token[j] < 0) continue;
-            score[j] = exp2_approx(score[j] - best);  // the weight from here on
+            // the weight from here on: differences are scaled, so that no finite score is too large to count
+            score[j] = exp2_approx((score[j] - best) * p.score_scale);
             sum += score[j];
             const int pos = token[j] - base;
             if (pos < 0 || pos >= p.slice) continue;

@@ -97,3 +97,31 @@ def test_parts_of_a_row_around_the_change_of_form():
             logits[1, 4000:4300] = (edge + part[1, 4000:4300]).float()
             logits[1, 4300:] = (edge - 20.0 - other[1, 4300:].abs()).float()
             check(ralm.knn_mix(logits, None, None, None, 0.5), reference(logits, None, None, None, 0.5, 1.0, 1.0, -1))
+
+
+def test_scores_of_any_size():
+    """Finite scores count, whatever they are and whatever the temperature makes of them; the tolerance holds for scores that
+    are large beside their differences too, as only the differences are scaled."""
+    ralm = _ralm()
+    R, V, k = 6, 97, 24
+    g = torch.Generator(DEV).manual_seed(5)
+    logits = torch.randn((R, V), generator=g, device=DEV)
+    ids, _, values = neighbours(R, V, k, 6)
+    near = 10.0 * torch.rand((R, k), generator=g, device=DEV)
+    for metric, sign in ((ralm.IP, 1), (ralm.L2, -1)):
+        for scores, tau in ((near + 1e4, 1.0), (near.round() + 1e6, 2.0), (near + 3e4, 10.0), (near - 2e4, 1.0),
+                            (torch.full_like(near, 1e30), 1e-10), (torch.full_like(near, -3e38), 1e-3), (near * 1e37, 1e-5),
+                            ((near - 5.0) * 6e37, 1.0), (near, 1e-37), (near, 3e38), (near * 1e37, 3e38)):
+            got = ralm.knn_mix(logits, ids, scores, values, 0.6, knn_temperature=tau, metric=metric)
+            check(got, reference(logits, ids, scores, values, 0.6, 1.0, tau, sign))
+
+
+def test_temperatures_whose_inverse_is_not_finite_are_refused():
+    ralm = _ralm()
+    logits, (ids, scores, values) = torch.randn((2, 50), device=DEV), neighbours(2, 50, 3, 7)
+    for bad in (dict(temperature=1e-39), dict(knn_temperature=1e-39), dict(temperature=4e-39), dict(knn_temperature=1e-45)):
+        with pytest.raises(ralm.RalmError) as e:
+            ralm.knn_mix(logits, ids, scores, values, 0.5, **bad)
+        assert e.value.status == 1
+    check(ralm.knn_mix(logits, ids, scores, values, 0.5, temperature=5e-39, knn_temperature=5e-39),
+          reference(logits, ids, scores, values, 0.5, 5e-39, 5e-39, -1))
