@@ -137,7 +137,8 @@ class Pages:
 
 class KVCache(Pages):
     """A key-value cache held in 4 bits (ralm_kv_t) over a page pool of kv_heads * page_size *
-    (head_dim + 8) bytes per page; head_dim 64 or 128, page_size 16, 32 or 64."""
+    (head_dim + 8) bytes per page; head_dim 64 or 128, page_size 16, 32 or 64. Attention's workspace (25 to 50 MB) is
+    made and cleared here, on the current stream; a call on another one comes after that, as with any tensor."""
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, *,
                  kv_heads: int, head_dim: int, page_size: int):
@@ -150,7 +151,9 @@ class KVCache(Pages):
         self._kv = _Kv(pages=self._c, kv_heads=kv_heads, head_dim=head_dim)
         self._kv_ptr = ctypes.addressof(self._kv)
         self._scale = head_dim ** -0.5
-        self._attend_work = {}      # (queries, heads) -> workspace
+        with torch.cuda.device(table.device):     # room for the partial results of split rows, whatever a call's sizes
+            size = max(self._lib.ralm_kv_attend_workspace(kv_heads, head_dim, kv_heads, n) for n in (8, 16, 24, 32))
+            self._attend_work = torch.zeros(size, dtype=torch.uint8, device=table.device)
 
     @staticmethod
     def page_bytes(kv_heads: int, head_dim: int, page_size: int) -> int:
@@ -165,8 +168,7 @@ class KVCache(Pages):
     def device_status(self, stream=None) -> int:
         status = super().device_status(stream)
         if status == 4:                                  # RALM_ERR_TIMEOUT: an attention call did not finish
-            for work in self._attend_work.values():
-                work.zero_()
+            self._attend_work.zero_()
         return status
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, count: torch.Tensor = None,
@@ -190,21 +192,5 @@ class KVCache(Pages):
                rows: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:
         """ralm_kv_attend: q [batch][n][q_heads][head_dim], the rows' newest n tokens -> out, the same shape
         and type. scale defaults to head_dim ** -0.5."""
-        work = self._attend_work.get(q.shape[1:3])
-        if work is None:
-            work = self._attend_workspace(q)
         return self._call.kv_attend(self._kv_ptr, layer, q, self._scale if scale is None else scale, q_len, rows, out,
-                                    work, stream)
-
-    def _attend_workspace(self, q: torch.Tensor) -> torch.Tensor:
-        """Room for the partial results of split rows, kept for later calls with as many queries and heads."""
-        if q.dim() != 4:
-            raise TypeError("q must be [batch][n][q_heads][%d]" % self.head_dim)
-        n, heads = q.shape[1:3]
-        with torch.cuda.device(self.table.device):
-            size = self._lib.ralm_kv_attend_workspace(self.kv_heads, self.head_dim, heads, n)
-        work = next((w for w in self._attend_work.values() if w.numel() >= size), None)
-        if work is None:
-            work = torch.zeros(max(size, 16), dtype=torch.uint8, device=self.table.device)
-        self._attend_work[q.shape[1:3]] = work
-        return work
+                                    self._attend_work, stream)
