@@ -7,6 +7,7 @@
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
+#include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <exception>
@@ -311,8 +312,8 @@ PyObject *pages_copy(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-ralm_kv_tokens_t kv_tokens(Args &args, const ralm_kv_t *c, PyObject *ko, PyObject *vo, PyObject *starts, PyObject *count, PyObject *rows) {
-    const at::Tensor &k = *args.tensor(ko, "k"), &v = *args.tensor(vo, "v");
+ralm_kv_tokens_t kv_tokens(Args &args, const ralm_kv_t *c, const at::Tensor &k, const at::Tensor &v, PyObject *starts, PyObject *count,
+                           PyObject *rows) {
     if (k.dim() != 4 || k.size(2) != c->kv_heads || k.size(3) != c->head_dim) throw Refused("k must be [batch][n][kv_heads][head_dim]");
     Args::shape(v, k.sizes(), "v");
     Args::type(v, k.scalar_type(), "v");
@@ -340,21 +341,45 @@ PyObject *kv_append(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const auto *c = static_cast<const ralm_kv_t *>(pointer(a[0]));
         Args args;
         args.tensor(a[8], "table");
-        const ralm_kv_tokens_t t = kv_tokens(args, c, a[2], a[3], a[4], a[5], a[6]);
+        const at::Tensor &k = *args.tensor(a[2], "k"), &v = *args.tensor(a[3], "v");
+        const ralm_kv_tokens_t t = kv_tokens(args, c, k, v, a[4], a[5], a[6]);
         Where w(args, a[7]);
         if (failed(calls.ralm_kv_append(c, int32(a[1], "layer"), &t, w.stream), "ralm_kv_append")) return nullptr;
         Py_RETURN_NONE;
     });
 }
+// cache, layer, k or None, v or None, starts, count, rows, stream, table, positions per entry, dtype of a k that is made here
 PyObject *kv_read(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return guarded(n, 9, [&]() -> PyObject * {
+    return guarded(n, 11, [&]() -> PyObject * {
         const auto *c = static_cast<const ralm_kv_t *>(pointer(a[0]));
         Args args;
         args.tensor(a[8], "table");
-        const ralm_kv_tokens_t t = kv_tokens(args, c, a[2], a[3], a[4], a[5], a[6]);
-        Where w(args, a[7]);
+        const at::Tensor *k = args.tensor(a[2], "k", true), *v = args.tensor(a[3], "v", true);
+        const at::Tensor &starts = *args.tensor(a[4], "starts");
+        const int32_t positions = int32(a[9], "n");
+        if (positions < 0) throw Refused("n must not be negative");
+        if (!THPDtype_Check(a[10])) throw Refused("dtype must be a torch.dtype");
+        if (starts.dim() != 1) throw Refused("starts must be [batch]");
+        if (k && (k->dim() != 4 || k->size(1) != positions)) throw Refused("k must be [batch][n][kv_heads][head_dim]");
+        Where w(args, a[7]);                                     // what is made here belongs to the call's stream
+        const int64_t shape[4] = {starts.size(0), positions, c->kv_heads, c->head_dim};
+        at::Tensor made_k, made_v;
+        if (!k) {
+            made_k = fresh(shape, reinterpret_cast<const THPDtype *>(a[10])->scalar_type, args.device);
+            k = &made_k;
+        }
+        if (!v) {
+            made_v = fresh(shape, k->scalar_type(), args.device);
+            v = &made_v;
+        }
+        const ralm_kv_tokens_t t = kv_tokens(args, c, *k, *v, a[4], a[5], a[6]);
         if (failed(calls.ralm_kv_read(c, int32(a[1], "layer"), &t, w.stream), "ralm_kv_read")) return nullptr;
-        return PyTuple_Pack(2, a[2], a[3]);
+        PyObject *first = made_k.defined() ? THPVariable_Wrap(made_k) : same(a[2]);
+        PyObject *second = made_v.defined() ? THPVariable_Wrap(made_v) : same(a[3]);
+        PyObject *both = PyTuple_Pack(2, first, second);
+        Py_DECREF(first);
+        Py_DECREF(second);
+        return both;
     });
 }
 

@@ -179,14 +179,9 @@ class KVCache(Pages):
 
     def read(self, layer: int, starts: torch.Tensor, n: int, dtype=torch.float16, k: torch.Tensor = None,
              v: torch.Tensor = None, count: torch.Tensor = None, rows: torch.Tensor = None, stream=None):
-        """ralm_kv_read: the values of positions starts .. starts + n - 1 -> (k, v) [batch][n][kv_heads][head_dim]."""
-        if k is None or v is None:
-            shape = (starts.shape[0], n, self.kv_heads, self.head_dim)
-            k = torch.empty(shape, dtype=dtype, device=starts.device) if k is None else k
-            v = torch.empty(shape, dtype=k.dtype, device=starts.device) if v is None else v
-        if k.dim() != 4 or k.shape[1] != n:
-            raise TypeError("k must be [batch][%d][kv_heads][head_dim]" % n)
-        return self._call.kv_read(self._kv_ptr, layer, k, v, starts, count, rows, stream, self.table)
+        """ralm_kv_read: the values of positions starts .. starts + n - 1 -> (k, v) [batch][n][kv_heads][head_dim], of
+        k's type where one is given."""
+        return self._call.kv_read(self._kv_ptr, layer, k, v, starts, count, rows, stream, self.table, n, dtype)
 
     def attend(self, layer: int, q: torch.Tensor, scale: float = None, q_len: torch.Tensor = None,
                rows: torch.Tensor = None, out: torch.Tensor = None, stream=None) -> torch.Tensor:

@@ -63,3 +63,28 @@ def test_first_attention_inside_a_capture():
     check(out, want, size)
     check(cache.attend(0, q), want, size)
     assert cache.device_status() == 0
+
+
+@pytest.mark.parametrize("given", ["neither", "k", "v"])
+def test_results_of_a_read_on_another_stream(given):
+    """Memory that queued work of the current stream still writes is not handed out for a result of another stream."""
+    cache, k, v, b = filled(2, 2, 64, 16, [90, 40], seed=3)
+    starts = i32([0, 0])
+    want = [x.clone() for x in cache.read(0, starts, 90)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):                  # loads the kernel, and leaves room in the other stream's allocator
+        cache.read(0, starts, 90)
+    own = torch.empty_like(want[0])
+    torch.cuda.synchronize()
+    blocks = [torch.empty_like(want[0]) for _ in range(4)]
+    done = busy()
+    for x in blocks:
+        x.fill_(7.0)                               # comes after the wait
+    del x, blocks                                  # free for the current stream to use again
+    got = cache.read(0, starts, 90, k=own if given == "k" else None, v=own if given == "v" else None, stream=side)
+    side.synchronize()
+    assert not done.query()
+    torch.cuda.synchronize()
+    for x, y in zip(got, want):
+        assert torch.equal(x, y)
+    assert got[0].dtype is torch.float16 and cache.device_status() == 0
