@@ -131,8 +131,10 @@ class Pages:
         self._call.pages_copy(other._ptr, src, self._ptr, dst, self.table, other.table, stream)
 
     def device_status(self, stream=None) -> int:
-        """ralm_pages_status: reads and clears the status word (synchronises)."""
-        return self._lib.ralm_pages_status(self._ptr, _stream_ptr(stream))
+        """ralm_pages_status: reads and clears the status word (synchronises `stream`, or the current stream of the
+        pool's device)."""
+        with torch.cuda.device(self.table.device):
+            return self._lib.ralm_pages_status(self._ptr, _stream_ptr(stream))
 
 
 class KVCache(Pages):
@@ -168,7 +170,8 @@ class KVCache(Pages):
     def device_status(self, stream=None) -> int:
         status = super().device_status(stream)
         if status == 4:                                  # RALM_ERR_TIMEOUT: an attention call did not finish
-            self._attend_work.zero_()
+            with torch.cuda.device(self.table.device), torch.cuda.stream(stream):
+                self._attend_work.zero_()
         return status
 
     def append(self, layer: int, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, count: torch.Tensor = None,
