@@ -132,13 +132,13 @@ template <int D> struct KvBlock {
         base = nullptr;
         inside = 0;
         slot = 0;
-        if (first >= count || first + 15 < 0) return;              // an entry's last block, not reached
+        const int lo = max(first, 0), hi = min(first + 16, count);  // the entry's tokens that the block takes
+        if (lo >= hi) return;                                       // none: nothing to refuse either
         const int row = kv_row(p, b);
         if (row < 0) return;
         inside = static_cast<int>(min(max(static_cast<int64_t>(kv_length(p, row)) - start, int64_t{0}), static_cast<int64_t>(count)));
-        const bool below = start < 0 && first < -start;             // positions before the row's first
-        if (write && (min(first + 16, count) > inside || below)) atomicMax(p.status, kStatusInvalid);
-        if (first >= inside || pos < 0) return;
+        if (write && (hi > inside || pos < 0)) atomicMax(p.status, kStatusInvalid);   // 0 is a block's first position
+        if (lo >= inside || pos < 0) return;
         const int page = p.table[static_cast<int64_t>(row) * p.max_pages + (pos >> p.page_shift)];
         if (page < 0 || page >= p.pages || (write && p.refs[page] != 1)) {   // a shared page is never written
             atomicMax(p.status, kStatusInvalid);
