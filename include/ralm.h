@@ -336,14 +336,14 @@ typedef enum { RALM_F16 = 0, RALM_BF16 = 1, RALM_F32 = 2 } ralm_dtype_t;
  *   ids, scores  [R][k] as ralm_search wrote them, 0 <= k <= RALM_MAX_K. An id outside [0, N), a value
  *           outside [0, V) and a score that is not finite are left out (padding of a short list).
  *   values  int32 [N], the token that follows each datastore entry.
- *   probs   fp32 [R][V], row pitch ld_probs (written); must not overlap the logits.
+ *   probs   fp32 [R][V], row pitch ld_probs (written); must not overlap the inputs.
  * A row with no neighbour left is softmax(logits / temperature) alone (k == 0 asks for just that), a
  * row whose logits are all -inf is the neighbours' distribution alone, a row with neither is zeros. A
  * NaN or +inf among the logits makes the row NaN, as in a softmax. Neighbours' weights are added in
  * fixed point: the result does not depend on the order of the atomics.
  * Errors: INVALID_ARG (null pointers, sizes, pitch < V, lambda outside [0, 1], temperatures that are not
  * positive and finite or below 4.3e-39, so that log2(e) over them is not finite, dtype or metric unknown,
- * logits == probs). R == 0 is a no-op. */
+ * probs overlapping an input). R == 0 is a no-op. */
 ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_logits, int32_t R, int32_t V,
                            const int64_t *ids, const float *scores, int32_t k, ralm_metric_t metric,
                            const int32_t *values, int64_t N, float lambda, float temperature,
@@ -365,7 +365,8 @@ ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_lo
  * t = floor(T * floor(2^24 u) / 2^24), it is the first v with w[0] + .. + w[v] > t. Whole numbers: the
  * token does not depend on how the row is split. If nothing is left of the difference the draw is
  * from target_probs[a]; if that row is empty too the token is -1.
- * Errors: INVALID_ARG. R == 0 is a no-op. */
+ * Errors: INVALID_ARG (null pointers, sizes, outputs that overlap inputs or one another: drafts are not
+ * verified in place). R == 0 is a no-op. */
 ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft_probs, int64_t draft_ld_r,
                                  int64_t draft_ld_s, const float *target_probs, int64_t target_ld_r,
                                  int64_t target_ld_s, const float *uniforms, const int32_t *draft_len, int32_t R,
@@ -461,7 +462,7 @@ ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_
  * entry is a decode step, drafts + 1 of them a verification. Queries that see nothing, and those at
  * or beyond q_len, give zeros.
  *   q, out   [batch][n][q_heads][head_dim], fp16 or bf16, strides in elements, last dimension contiguous; they
- *            must not overlap (q == out is refused);
+ *            must not overlap (INVALID_ARG);
  *            q_heads a multiple of kv_heads, query head h reads key-value head h / (q_heads / kv_heads).
  *   workspace of ralm_kv_attend_workspace(...) bytes, 16-byte aligned, ZEROED by the caller before its first
  *            use; calls of any sizes may follow one another in it, one at a time. */

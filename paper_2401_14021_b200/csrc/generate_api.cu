@@ -8,6 +8,8 @@
 #include <algorithm>
 #include <atomic>
 #include <cmath>
+#include <initializer_list>
+#include <utility>
 
 #include "attend.cuh"
 #include "kv4.cuh"
@@ -20,6 +22,45 @@ using namespace ralm;
 namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+
+// Where the elements of a strided argument lie: runs of contiguous bytes, n[i] of them step[i] bytes apart, the longest
+// step first.
+struct Runs {
+    int64_t at, bytes, n[3], step[3], extent[4];   // extent[i]: from the first byte to the end of dimensions i and on
+    Runs(const void *p, int64_t bytes_, std::initializer_list<std::pair<int64_t, int64_t>> dims)
+        : at(static_cast<int64_t>(reinterpret_cast<uintptr_t>(p))), bytes(p ? bytes_ : 0) {
+        int d = 0;
+        for (auto [count, stride] : dims) {
+            if (count <= 0) bytes = 0;
+            if (stride < 0) at += (count - 1) * stride;
+            const int64_t s = stride < 0 ? -stride : stride, c = s == 0 ? 1 : count;
+            int i = d++;
+            for (; i > 0 && step[i - 1] < s; --i) n[i] = n[i - 1], step[i] = step[i - 1];
+            n[i] = c;
+            step[i] = s;
+        }
+        for (; d < 3; ++d) n[d] = 1, step[d] = 0;
+        extent[3] = bytes;
+        for (int i = 2; i >= 0; --i) extent[i] = extent[i + 1] + (n[i] - 1) * step[i];
+    }
+    static bool meet(const Runs &a, int i, int64_t pa, const Runs &b, int j, int64_t pb) {
+        const int64_t ea = a.extent[i], eb = b.extent[j];
+        if (pa + ea <= pb || pb + eb <= pa) return false;
+        while (i < 3 && a.n[i] == 1) ++i;
+        while (j < 3 && b.n[j] == 1) ++j;
+        if (i == 3 && j == 3) return true;
+        if (i == 3 || (j < 3 && eb > ea)) return meet(b, j, pb, a, i, pa);
+        // those parts of a that reach into b's range
+        const int64_t s = a.step[i], part = a.extent[i + 1];
+        const int64_t first = pb - part - pa < 0 ? 0 : (pb - part - pa) / s + 1, last = std::min(a.n[i] - 1, (pb + eb - 1 - pa) / s);
+        for (int64_t k = first; k <= last; ++k)
+            if (meet(a, i + 1, pa + k * s, b, j, pb)) return true;
+        return false;
+    }
+    // Whether the two share a byte. Arguments in different places, the usual ones, are told apart at once.
+    bool overlaps(const Runs &o) const { return bytes > 0 && o.bytes > 0 && meet(*this, 0, at, o, 0, o.at); }
+};
+Runs dense(const void *p, int64_t bytes) { return Runs(p, bytes, {}); }
 
 // SMs of the current device (0: none), asked once per device.
 int sm_count() {
@@ -249,9 +290,14 @@ ralm_status_t ralm_knn_mix(const void *logits, ralm_dtype_t dtype, int64_t ld_lo
         std::isinf(knn_temperature) || std::isinf(kLog2e / temperature) || std::isinf(kLog2e / knn_temperature))
         return RALM_ERR_INVALID_ARG;
     if (R == 0) return RALM_OK;
-    if (!logits || !probs || logits == probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
-    if (reinterpret_cast<uintptr_t>(logits) % (dtype == RALM_F32 ? 4 : 2) != 0) return RALM_ERR_INVALID_ARG;
+    if (!logits || !probs || (k > 0 && (!ids || !scores || (N > 0 && !values)))) return RALM_ERR_INVALID_ARG;
+    const int64_t size = dtype == RALM_F32 ? 4 : 2;
+    if (reinterpret_cast<uintptr_t>(logits) % size != 0) return RALM_ERR_INVALID_ARG;
     if (static_cast<int64_t>(R) * kMixMaxCluster >= (int64_t{1} << 31)) return RALM_ERR_INVALID_ARG;
+    const Runs written(probs, 4 * static_cast<int64_t>(V), {{R, 4 * ld_probs}});
+    if (written.overlaps(Runs(logits, size * V, {{R, size * ld_logits}})) || written.overlaps(dense(ids, 8LL * R * k)) ||
+        written.overlaps(dense(scores, 4LL * R * k)) || (k > 0 && written.overlaps(dense(values, 4 * N))))
+        return RALM_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return RALM_ERR_CUDA;
     MixParams p;
@@ -284,6 +330,15 @@ ralm_status_t ralm_verify_tokens(const int64_t *draft_tokens, const float *draft
     if (R == 0) return RALM_OK;
     if ((S > 0 && !draft_tokens) || !target_probs || !uniforms || !tokens || !accepted) return RALM_ERR_INVALID_ARG;
     if (static_cast<int64_t>(R) * kVtMaxCluster >= (int64_t{1} << 31)) return RALM_ERR_INVALID_ARG;
+    // the CTAs of a request all read its inputs, and one of them writes its outputs while they do
+    const Runs out[2] = {dense(tokens, 8LL * R * (S + 1)), dense(accepted, 4LL * R)};
+    if (out[0].overlaps(out[1])) return RALM_ERR_INVALID_ARG;
+    for (const Runs &o : out)
+        if (o.overlaps(dense(draft_tokens, 8LL * R * S)) || o.overlaps(dense(uniforms, 4LL * R * (S + 1))) ||
+            o.overlaps(dense(draft_len, 4LL * R)) ||
+            o.overlaps(Runs(draft_probs, 4LL * V, {{R, 4 * draft_ld_r}, {S, 4 * draft_ld_s}})) ||
+            o.overlaps(Runs(target_probs, 4LL * V, {{R, 4 * target_ld_r}, {S + 1LL, 4 * target_ld_s}})))
+            return RALM_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return RALM_ERR_CUDA;
     VerifyTokensParams p;
@@ -399,7 +454,10 @@ ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_a
         return RALM_ERR_INVALID_ARG;
     if (cache->head_dim != 64 && cache->head_dim != 128) return RALM_ERR_UNSUPPORTED;
     if (a->batch == 0 || a->n == 0) return RALM_OK;
-    if (!a->q || !a->out || a->q == a->out || !a->workspace || !aligned16(a->workspace)) return RALM_ERR_INVALID_ARG;
+    if (!a->q || !a->out || !a->workspace || !aligned16(a->workspace)) return RALM_ERR_INVALID_ARG;
+    if (Runs(a->out, 2LL * cache->head_dim, {{a->batch, 2 * a->out_stride_b}, {a->n, 2 * a->out_stride_n}, {a->q_heads, 2 * a->out_stride_h}})
+            .overlaps(Runs(a->q, 2LL * cache->head_dim, {{a->batch, 2 * a->q_stride_b}, {a->n, 2 * a->q_stride_n}, {a->q_heads, 2 * a->q_stride_h}})))
+        return RALM_ERR_INVALID_ARG;
     const int group = a->q_heads / cache->kv_heads;
     const int64_t rows = static_cast<int64_t>(group) * a->n;
     const ralm_pages_t &pg = cache->pages;
