@@ -193,7 +193,7 @@ PagesCopyParams copy_in_pool(const ralm_pages_t &p) {
 bool kv_ok(const ralm_kv_t *c, int32_t layer) {
     if (!c || !pages_ok(&c->pages) || !pool_ok(&c->pages)) return false;
     const ralm_pages_t &p = c->pages;
-    return c->kv_heads >= 1 && c->kv_heads <= 4096 && (p.page_size == 16 || p.page_size == 32 || p.page_size == 64) && layer >= 0 &&
+    return p.pages >= 1 && c->kv_heads >= 1 && c->kv_heads <= 4096 && (p.page_size == 16 || p.page_size == 32 || p.page_size == 64) && layer >= 0 &&
            layer < p.layers && p.page_bytes == static_cast<int64_t>(c->kv_heads) * p.page_size * (c->head_dim + 8);
 }
 KvParams kv_params(const ralm_kv_t &c, int32_t layer, const int32_t *rows, int batch) {
