@@ -551,6 +551,7 @@ attend_kernel(const AttendParams p) {
     __shared__ __align__(8) int scratch[64];
     __shared__ __align__(8) uint64_t bars[WARPS * STAGES];
     __shared__ int2 open_piece[WARPS], left_piece[WARPS];
+    __shared__ __align__(8) float row_factor[WARPS][ROWS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, g = lane >> 2, t = lane & 3;
     unsigned char *ring = attend_smem + warp * attend_warp_bytes(NT, D);
     uint4 *q_smem = reinterpret_cast<uint4 *>(ring + STAGES * STAGE);
@@ -650,10 +651,14 @@ attend_kernel(const AttendParams p) {
         float qsum[NT][2];
         int last[NT][2];                 // the newest key that columns 2 t and 2 t + 1 see
         float f = 1.f;
+        int all_see;                     // the newest key that all columns see alike; -1: some column is no query, or has a factor
         {
-            // bring the rows to [2^10, 2^11) by one power of two: bf16 fits fp16, and 16 q does too
+            // bring the rows to [2^10, 2^11) by a power of two: bf16 fits fp16, and 16 q does too. One power for the rows of
+            // a pass, which then share the keys' scales, unless a row lies more than 2^10 below the largest or that one above
+            // 2^51 (where the common factor would leave fp32's range): such a row gets its own, and its scores a factor.
+            // Within the 2^10 a row is rounded at 2^-25 of its own largest value at worst.
             union Eight { uint4 raw; T x[8]; } u[NT][W];
-            float top = 0.f;
+            float row_top[NT], top = 0.f;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int qr = seg.rb * ROWS + nt * 8 + g;
@@ -661,6 +666,7 @@ attend_kernel(const AttendParams p) {
                 const int i = real ? qr / p.group : 0, gq = real ? qr - i * p.group : 0;
                 const T *src = static_cast<const T *>(p.q) + seg.b * p.q_b + i * p.q_n +
                                (static_cast<int64_t>(seg.h) * p.group + gq) * p.q_h + t * (D / 4);
+                row_top[nt] = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
                     u[nt][w].raw = make_uint4(0, 0, 0, 0);
@@ -670,15 +676,36 @@ attend_kernel(const AttendParams p) {
 #pragma unroll
                             for (int j = 0; j < 8; ++j) u[nt][w].x[j] = src[8 * w + j];
                     }
-                    top = fmaxf(top, q_top(u[nt][w].x));
+                    row_top[nt] = fmaxf(row_top[nt], q_top(u[nt][w].x));
                 }
+                row_top[nt] = fmaxf(row_top[nt], __shfl_xor_sync(0xffffffffu, row_top[nt], 1));
+                row_top[nt] = fmaxf(row_top[nt], __shfl_xor_sync(0xffffffffu, row_top[nt], 2));
+                top = fmaxf(top, row_top[nt]);
             }
-            top = warp_max(top);
-            const int e = top > 0.f ? min(max(static_cast<int>(__float_as_uint(top) >> 23) - 127 - 10, -100), 117) : 0;
+            top = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top)));     // not negative: bits have its order
+            auto power = [](float x) { return min(max(static_cast<int>(__float_as_uint(x) >> 23) - 127 - 10, -126), 117); };
+            const int e = top > 0.f ? min(power(top), 40) : 0;
+            auto row_power = [&](float x) {
+                const int r = x > 0.f ? max(power(x), e - 120) : e;
+                return r <= e && r >= e - 10 ? e : r;
+            };
             f = __uint_as_float((127 + e) << 23);
-            const float inv = __uint_as_float((127 - e) << 23);
+            bool own = false;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) own |= row_power(row_top[nt]) != e;
+            const bool spread = __any_sync(0xffffffffu, own);
+            all_see = n < p.n || spread ? -1 : len - n;
+            __syncwarp();                // the last segment's factors have been read
+            float inv = __uint_as_float((127 - e) << 23);
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
+                float by = 1.f;
+                if (spread) {
+                    const int r = row_power(row_top[nt]);
+                    inv = __uint_as_float((127 - r) << 23);
+                    by = __uint_as_float((127 + r - e) << 23);
+                }
+                if (t == 0) row_factor[warp][nt * 8 + g] = by;
                 float sum = 0.f;
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
@@ -699,6 +726,7 @@ attend_kernel(const AttendParams p) {
                 }
                 sum += __shfl_xor_sync(0xffffffffu, sum, 1);
                 sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+                sum *= by;
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     qsum[nt][c] = __shfl_sync(0xffffffffu, sum, (2 * t + c) * 4);
@@ -707,6 +735,7 @@ attend_kernel(const AttendParams p) {
                 }
             }
         }
+        __syncwarp();                    // the factors are in place
         f *= p.scale * 1048576.f;        // the codes' 2^-20
 
         // acc is in units of 2^-24 or 2^-20 / v_unit, the weights are 2^(score - mb), mb a maximum less kAttendBias
@@ -739,7 +768,8 @@ attend_kernel(const AttendParams p) {
             ++done;
             const int tok0 = (seg.unit + u) << share.shift;
             const unsigned char *st = ring + slot * STAGE;
-            // tiles of 16 tokens, side by side where all queries see all of them; MASKED: one that some query does not
+            // tiles of 16 tokens, side by side where all queries see all of them and share a power of two; MASKED: one
+            // where that does not hold
             auto tile = [&](auto masked_type, int h) {
                 constexpr bool masked = decltype(masked_type)::value;
                 constexpr int KT = masked ? 1 : TILES;
@@ -787,6 +817,17 @@ attend_kernel(const AttendParams p) {
                             else q4 = q_smem[(nt * W + w) * 32 + lane];
                             mma_f16(sc[kt][nt], a[0], b[0], a[1], b[1], q4.x, q4.y);
                             mma_f16(sc[kt][nt], a[2], b[2], a[3], b[3], q4.z, q4.w);
+                        }
+                    }
+                }
+                if (masked) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) {
+                        const float2 by = *reinterpret_cast<const float2 *>(&row_factor[warp][nt * 8 + 2 * t]);
+#pragma unroll
+                        for (int kt = 0; kt < KT; ++kt) {
+                            sc[kt][nt][0] *= by.x, sc[kt][nt][2] *= by.x;
+                            sc[kt][nt][1] *= by.y, sc[kt][nt][3] *= by.y;
                         }
                     }
                 }
@@ -898,7 +939,7 @@ attend_kernel(const AttendParams p) {
             const int tiles = (min(unit_tokens, len - tok0) + 15) >> 4;
 #pragma unroll 1
             for (int h = 0; h < tiles;) {
-                if (h + TILES > tiles || tok0 + 16 * (h + TILES) - 1 > len - n || n < p.n) tile(std::true_type{}, h), ++h;
+                if (h + TILES > tiles || tok0 + 16 * (h + TILES) - 1 > all_see) tile(std::true_type{}, h), ++h;
                 else tile(std::false_type{}, h), h += TILES;
             }
             __syncwarp();                // the stage has been read: it may be overwritten

@@ -450,7 +450,7 @@ int64_t ralm_kv_attend_workspace(int32_t kv_heads, int32_t head_dim, int32_t q_h
 
 ralm_status_t ralm_kv_attend(const ralm_kv_t *cache, int32_t layer, const ralm_attend_t *a, void *stream) {
     if (!kv_ok(cache, layer) || !a || a->batch < 0 || a->batch > RALM_MAX_ATTEND_BATCH || a->n < 0 || a->q_heads < 1 ||
-        a->q_heads % cache->kv_heads != 0 || (a->dtype != RALM_F16 && a->dtype != RALM_BF16) || !std::isfinite(a->scale))
+        a->q_heads % cache->kv_heads != 0 || (a->dtype != RALM_F16 && a->dtype != RALM_BF16) || !std::isfinite(a->scale * kLog2e))
         return RALM_ERR_INVALID_ARG;
     if (cache->head_dim != 64 && cache->head_dim != 128) return RALM_ERR_UNSUPPORTED;
     if (a->batch == 0 || a->n == 0) return RALM_OK;
