@@ -3,12 +3,13 @@
 //
 // With k = s_k (c - 8) + b_k the score is s_k q.c + (b_k - 8 s_k) sum(q), and the output is
 // sum (p s_v)(c - 8) + sum p b_v: the matrix instructions see whole numbers, and the scales enter in 32 bits.
-// A code needs no conversion: four bits in the lowest places of an fp16 word ARE the number c 2^-24, and in
-// the next four c 2^-20, subnormals that the instructions take exactly. One masking instruction makes an
-// operand of two codes; the powers of two go into q and the results. The 8 matters in the second product
-// only, where thousands of weights would pile up 7.5 times their sum beside a small difference: it is taken
-// from the operand (one instruction, shared by all query rows), or with a single block of 8 query rows by a
-// second product of the weights with a constant -8, which the matrix pipe has time for.
+// For the first product a code needs no conversion: four bits in the lowest places of an fp16 word ARE the number
+// c 2^-24, and in the next four c 2^-20, subnormals that the instructions take exactly. One masking instruction makes an
+// operand of two codes; the powers of two go into q and the results. The instructions line addends up by their exponents,
+// and a subnormal's counts as 2^-14: sums keep 2^-14 of a step of the code times the largest |q|, measured 2^-23.1 of
+// sum |q c| at worst over 128 dimensions (2^-24.2 with normal numbers, one more instruction an operand).
+// In the second product the addends differ by far more, by the weights of a softmax: there the operand is c - 8 as a normal
+// number, two instructions shared by all query rows, and what is small beside the largest weight of a tile is not cut off.
 // The weights p s_v are rounded to fp16 (11 bits) before the second product; maxima, sums and outputs stay in
 // 32 bits.
 //
@@ -115,12 +116,23 @@ __device__ __forceinline__ void unpack4(uint32_t x, uint32_t (&y)[4]) {
     y[3] = z & 0x00F000F0u;
 }
 
-// The same as c - 8: exact, the difference of two multiples of 2^-24.
-__device__ __forceinline__ void unpack4_centred(uint32_t x, uint32_t (&y)[4]) {
-    unpack4(x, y);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) y[i] = hsub2(y[i], i % 2 == 0 ? 0x00080008u : 0x00800080u);
-}
+// c - 8 of the same pairs, as normal numbers: 1024 + c and 64 + c are a mask and an exponent away, the difference is exact.
+// The exponents come out of a shuffle so that the compiler holds them in ordinary registers, where mask and exponent are
+// one instruction (32 x 8 heads of 2000 to 32000 tokens: 129 us, 138 with two).
+struct Centre {
+    uint32_t e1024, e64;
+    __device__ __forceinline__ Centre() {
+        e1024 = __shfl_sync(0xffffffffu, 0x64006400u, threadIdx.x & 31);
+        e64 = __shfl_sync(0xffffffffu, 0x54005400u, threadIdx.x & 31);
+    }
+    __device__ __forceinline__ void unpack4(uint32_t x, uint32_t (&y)[4]) const {
+        const uint32_t z = x >> 8;
+        y[0] = hsub2((x & 0x000F000Fu) | e1024, 0x64086408u);
+        y[1] = hsub2((x & 0x00F000F0u) | e64, 0x54805480u);
+        y[2] = hsub2((z & 0x000F000Fu) | e1024, 0x64086408u);
+        y[3] = hsub2((z & 0x00F000F0u) | e64, 0x54805480u);
+    }
+};
 
 // The largest finite absolute value of eight; infinities and NaN do not set a row's scale.
 __device__ __forceinline__ float q_top(const __half *x) {
@@ -632,6 +644,7 @@ attend_kernel(const AttendParams p) {
             if (feed.seg.b != b) feed.enter(p);
         }
     };
+    const Centre centre;
     Segment seg = mine_first;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) issue();
@@ -738,7 +751,7 @@ attend_kernel(const AttendParams p) {
         __syncwarp();                    // the factors are in place
         f *= p.scale * 1048576.f;        // the codes' 2^-20
 
-        // acc is in units of 2^-24 or 2^-20 / v_unit, the weights are 2^(score - mb), mb a maximum less kAttendBias
+        // acc is in units of 1 / v_unit, the weights are 2^(score - mb), mb a maximum less kAttendBias
         float acc[NT][MT][4], mb[NT][2], l[NT][2], ob[NT][2];
         float v_unit = 1.f, v_limit = 0.f;
 #pragma unroll
@@ -922,16 +935,12 @@ attend_kernel(const AttendParams p) {
                             const uint32_t pick = half ? 0x7632 : 0x5410;
                             const uint32_t xa = __byte_perm(xv[kt][0].w[w], xv[kt][0].w[W / 2 + w], pick);
                             const uint32_t xb = __byte_perm(xv[kt][1].w[w], xv[kt][1].w[W / 2 + w], pick);
-                            if (NT == 1) unpack4(xa, a), unpack4(xb, b);
-                            else unpack4_centred(xa, a), unpack4_centred(xb, b);
+                            centre.unpack4(xa, a);
+                            centre.unpack4(xb, b);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_f16(acc[nt][4 * w + 2 * half], a[0], a[1], b[0], b[1], pf[kt][nt][0], pf[kt][nt][1]);
                                 mma_f16(acc[nt][4 * w + 2 * half + 1], a[2], a[3], b[2], b[3], pf[kt][nt][0], pf[kt][nt][1]);
-                            }
-                            if (NT == 1) {
-                                mma_f16(acc[0][4 * w + 2 * half], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pf[kt][0][0], pf[kt][0][1]);
-                                mma_f16(acc[0][4 * w + 2 * half + 1], 0x80088008u, 0x80808080u, 0x80088008u, 0x80808080u, pf[kt][0][0], pf[kt][0][1]);
                             }
                         }
                     }
@@ -966,7 +975,7 @@ attend_kernel(const AttendParams p) {
             if (seg.unit == 0) open_piece[warp] = make_int2(1, segment);
             else left_piece[warp] = make_int2(seg.unit + mine == seg.units ? 2 : 1, segment);
         }
-        const float v_back = 1.f / v_unit, lo_back = 16777216.f * v_back, hi_back = 1048576.f * v_back;
+        const float v_back = 1.f / v_unit;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -978,15 +987,15 @@ attend_kernel(const AttendParams p) {
                     T *o = attend_row<T>(p, seg, qr);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        o[16 * i + g] = from_float<T>(fmaf(acc[nt][i][e], lo_back, ob[nt][e]) * inv);
-                        o[16 * i + 8 + g] = from_float<T>(fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]) * inv);
+                        o[16 * i + g] = from_float<T>(fmaf(acc[nt][i][e], v_back, ob[nt][e]) * inv);
+                        o[16 * i + 8 + g] = from_float<T>(fmaf(acc[nt][i][2 + e], v_back, ob[nt][e]) * inv);
                     }
                 } else {
                     float *o = near ? reinterpret_cast<float *>(ring) + lr * attend_row_floats(D) : p.part + (piece * ROWS + lr) * D;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        o[16 * i + g] = fmaf(acc[nt][i][e], lo_back, ob[nt][e]);
-                        o[16 * i + 8 + g] = fmaf(acc[nt][i][2 + e], hi_back, ob[nt][e]);
+                        o[16 * i + g] = fmaf(acc[nt][i][e], v_back, ob[nt][e]);
+                        o[16 * i + 8 + g] = fmaf(acc[nt][i][2 + e], v_back, ob[nt][e]);
                     }
                     if (g == 0) {
                         float *ml = near ? o + D : p.part_ml + (piece * ROWS + lr) * 2;

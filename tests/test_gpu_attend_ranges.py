@@ -42,3 +42,26 @@ def test_a_row_does_not_depend_on_its_neighbours_size(D, n, G, factor):
         scaled = (q * x).bfloat16()
         s = D ** -0.5 / x
         check(cache.attend(0, scaled, scale=s), *attend_reference(scaled, dk, dv, bv, lengths, s))
+
+
+# ---- weights of very different sizes
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,G", [(1, 1), (1, 8), (2, 8), (3, 8), (4, 8)])
+@pytest.mark.parametrize("gap", [6.0, 9.0, 12.0, 16.0])
+def test_small_weights_count_where_the_largest_stands_for_nothing(D, n, G, gap):
+    """Where the token with nearly all the weight stands for exactly 0, the others are the result, though their weights are
+    exp(-gap) of its."""
+    cache, order = make_cache(1, 1, D, 16, 4, seed=4)
+    give_pages(cache, order, [48 + n])
+    g = torch.Generator(DEV).manual_seed(int(gap))
+    k = torch.randn((1, 48 + n, 1, D), generator=g, device=DEV)
+    k = 0.5 * (k - k.mean(-1, keepdim=True))                     # scores of 0
+    v = 0.2 * torch.randn((1, 48 + n, 1, D), generator=g, device=DEV)
+    k[0, 21] = 1.0                                               # a score of gap
+    v[0, 21], v[0, 21, 0, 0], v[0, 21, 0, 1] = 0.0, -2.0, 1.75   # steps of 0.25, no offset
+    k, v = k.half(), v.half()
+    cache.append(0, k, v, i32([0]))
+    (dk, _), (dv, bv) = values_of(k), values_of(v)
+    assert (dv[0, 21, 0, 2:] == 0).all() and (bv[0, 21] == 0).all()
+    q = torch.ones((1, n, G, D), device=DEV).half()
+    check(cache.attend(0, q, scale=gap / D), *attend_reference(q, dk, dv, bv, [48 + n], gap / D))
