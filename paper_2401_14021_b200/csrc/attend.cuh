@@ -11,7 +11,9 @@
 // In the second product the addends differ by far more, by the weights of a softmax: there the operand is c - 8 as a normal
 // number, two instructions shared by all query rows, and what is small beside the largest weight of a tile is not cut off.
 // The weights p s_v are rounded to fp16 (11 bits) before the second product; maxima, sums and outputs stay in
-// 32 bits.
+// 32 bits. What p is relative to is, for each query row, the largest p s_v, not the largest p: so the weights that
+// count lie high in fp16's range, whatever the sizes of the values, and one large value that does not count for a
+// row costs it nothing (2^22 lie between the largest weight and the first that loses bits).
 //
 // A warp is a worker with its own stages in shared memory (bulk copies of 32 tokens, completion on a
 // barrier of its own): no warp waits for another, and any mix of lengths keeps all of them busy.
@@ -47,7 +49,7 @@ namespace ralm {
 constexpr int kAttendMaxBatch = 4096;
 constexpr int kAttendStage = 64;         // tokens of a stage in shared memory, the largest unit of work
 constexpr float kAttendLazy = 6.f;       // a maximum may be this far (powers of two) behind before sums are rescaled
-constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8 + 1) is below fp16's largest
+constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8) (and 2^0.1 for log2_of_half) is below fp16's largest
 
 // Warps per CTA (one CTA per SM) and whether the query operands stay in registers, by column blocks.
 __host__ __device__ constexpr int attend_warps(int nt, int d) { return nt >= 3 ? 8 : nt == 1 && d == 64 ? 16 : 12; }
@@ -133,6 +135,12 @@ struct Centre {
         y[3] = hsub2((z & 0x00F000F0u) | e64, 0x54805480u);
     }
 };
+
+// log2 of the fp16 number in the low half of a word, within 0.09 below; up to 9 above for subnormals, -15 for zero. Its bits
+// are a number of 1024ths; put behind those of 2^23 they are one in fp32.
+__device__ __forceinline__ float log2_of_half(uint32_t pair) {
+    return fmaf(__uint_as_float(__byte_perm(pair, 0x4B000000u, 0x7610)), 1.f / 1024.f, -8207.f);   // 2^23 / 1024 + 15
+}
 
 // The largest finite absolute value of eight; infinities and NaN do not set a row's scale.
 __device__ __forceinline__ float q_top(const __half *x) {
@@ -751,9 +759,8 @@ attend_kernel(const AttendParams p) {
         __syncwarp();                    // the factors are in place
         f *= p.scale * 1048576.f;        // the codes' 2^-20
 
-        // acc is in units of 1 / v_unit, the weights are 2^(score - mb), mb a maximum less kAttendBias
+        // the weights are 2^(score - mb), mb a maximum of score + log2 s_v less kAttendBias
         float acc[NT][MT][4], mb[NT][2], l[NT][2], ob[NT][2];
-        float v_unit = 1.f, v_limit = 0.f;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
@@ -788,7 +795,7 @@ attend_kernel(const AttendParams p) {
                 constexpr int KT = masked ? 1 : TILES;
                 const int tok = tok0 + 16 * h;
                 LaneCodes<D> xk[KT][2], xv[KT][2];
-                float ks[KT][2], kb[KT][2], vs[KT][2], vb[KT][2];
+                float ks[KT][2], kb[KT][2], vs[KT][2], vb[KT][2], vl[KT][2];
 #pragma unroll
                 for (int kt = 0; kt < KT; ++kt) {
                     const int at = tok + 16 * kt;
@@ -800,11 +807,13 @@ attend_kernel(const AttendParams p) {
                         load_codes<D>(xk[kt][j], codes + j * (4 * D));
                         load_codes<D>(xv[kt][j], codes + ps * (D / 2) + j * (4 * D));
                         const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(pairs + j * 32));
-                        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(pairs + ps * 4 + j * 32));
+                        const uint32_t v_pair = *reinterpret_cast<const uint32_t *>(pairs + ps * 4 + j * 32);
+                        const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&v_pair));
                         ks[kt][j] = a.x * f;
                         kb[kt][j] = (a.y - 8.f * a.x) * (f * 9.5367431640625e-7f);        // sum(q) carries no 2^-20
                         vs[kt][j] = b.x;
                         vb[kt][j] = b.y;
+                        vl[kt][j] = log2_of_half(v_pair);
                         if (masked && at + g + 8 * j >= len) vs[kt][j] = vb[kt][j] = 0.f;   // the rest of a page holds anything
                     }
                 }
@@ -845,34 +854,25 @@ attend_kernel(const AttendParams p) {
                     }
                 }
                 float pr[KT][NT][4];
-                float ahead = -INFINITY, v_top = 0.f;
+                float ahead = -INFINITY;
 #pragma unroll
-                for (int kt = 0; kt < KT; ++kt) {
-                    v_top = fmaxf(v_top, fmaxf(vs[kt][0], vs[kt][1]));
+                for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int j = 0; j < 2; ++j) {
+                        float key = -INFINITY;
 #pragma unroll
-                        for (int j = 0; j < 2; ++j)
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                             for (int e = 0; e < 2; ++e) {
                                 float v = fmaf(ks[kt][j], sc[kt][nt][2 * j + e], fmaf(kb[kt][j], qsum[nt][e], -mb[nt][e]));
                                 if (masked && tok + 16 * kt + g + 8 * j > last[nt][e]) v = -INFINITY;
                                 pr[kt][nt][2 * j + e] = v;
-                                ahead = fmaxf(ahead, v);
+                                key = fmaxf(key, v);
                             }
-                }
-                if (__any_sync(0xffffffffu, ahead > kAttendLazy + kAttendBias || v_top >= v_limit)) {
-                    // a new maximum, or V scales beyond the unit: bring the sums to the new reference
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) v_top = fmaxf(v_top, __shfl_xor_sync(0xffffffffu, v_top, o));
-                    float ratio = 1.f;
-                    if (v_top >= v_limit && v_top > 0.f) {
-                        const int e = static_cast<int>(__float_as_uint(v_top) >> 23) - 127;   // fp16: -24 .. 15
-                        const float unit = __uint_as_float((127 - e) << 23);
-                        ratio = unit / v_unit;
-                        v_unit = unit;
-                        v_limit = __uint_as_float((127 + e + 1) << 23);
+                        ahead = fmaxf(ahead, key + vl[kt][j]);
                     }
+                if (__any_sync(0xffffffffu, ahead > kAttendLazy + kAttendBias)) {
+                    // a new maximum: bring the sums to the new reference
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -885,7 +885,7 @@ attend_kernel(const AttendParams p) {
                                     float v = fmaf(ks[kt][j], sc[kt][nt][2 * j + e], kb[kt][j] * qsum[nt][e]);
                                     if (masked && tok + 16 * kt + g + 8 * j > last[nt][e]) v = -INFINITY;
                                     pr[kt][nt][2 * j + e] = v;
-                                    top = fmaxf(top, v);
+                                    top = fmaxf(top, v + vl[kt][j]);
                                 }
                             top -= kAttendBias;
 #pragma unroll
@@ -895,11 +895,10 @@ attend_kernel(const AttendParams p) {
                             mb[nt][e] = now;
                             l[nt][e] *= by;
                             ob[nt][e] *= by;
-                            const float by_acc = by * ratio;
 #pragma unroll
                             for (int i = 0; i < MT; ++i) {
-                                acc[nt][i][e] *= by_acc;
-                                acc[nt][i][2 + e] *= by_acc;
+                                acc[nt][i][e] *= by;
+                                acc[nt][i][2 + e] *= by;
                             }
 #pragma unroll
                             for (int kt = 0; kt < KT; ++kt)
@@ -912,7 +911,6 @@ attend_kernel(const AttendParams p) {
                 for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
                     for (int j = 0; j < 2; ++j) {
-                        const float vu = vs[kt][j] * v_unit;
 #pragma unroll
                         for (int nt = 0; nt < NT; ++nt) {
                             const float p0 = exp2_approx(pr[kt][nt][2 * j]), p1 = exp2_approx(pr[kt][nt][2 * j + 1]);
@@ -920,7 +918,7 @@ attend_kernel(const AttendParams p) {
                             l[nt][1] += p1;
                             ob[nt][0] = fmaf(p0, vb[kt][j], ob[nt][0]);
                             ob[nt][1] = fmaf(p1, vb[kt][j], ob[nt][1]);
-                            const __half2 hp = __floats2half2_rn(p0 * vu, p1 * vu);
+                            const __half2 hp = __floats2half2_rn(p0 * vs[kt][j], p1 * vs[kt][j]);
                             pf[kt][nt][j] = transpose8x8(*reinterpret_cast<const uint32_t *>(&hp));
                         }
                     }
@@ -975,7 +973,6 @@ attend_kernel(const AttendParams p) {
             if (seg.unit == 0) open_piece[warp] = make_int2(1, segment);
             else left_piece[warp] = make_int2(seg.unit + mine == seg.units ? 2 : 1, segment);
         }
-        const float v_back = 1.f / v_unit;
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -987,15 +984,15 @@ attend_kernel(const AttendParams p) {
                     T *o = attend_row<T>(p, seg, qr);
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        o[16 * i + g] = from_float<T>(fmaf(acc[nt][i][e], v_back, ob[nt][e]) * inv);
-                        o[16 * i + 8 + g] = from_float<T>(fmaf(acc[nt][i][2 + e], v_back, ob[nt][e]) * inv);
+                        o[16 * i + g] = from_float<T>((acc[nt][i][e] + ob[nt][e]) * inv);
+                        o[16 * i + 8 + g] = from_float<T>((acc[nt][i][2 + e] + ob[nt][e]) * inv);
                     }
                 } else {
                     float *o = near ? reinterpret_cast<float *>(ring) + lr * attend_row_floats(D) : p.part + (piece * ROWS + lr) * D;
 #pragma unroll
                     for (int i = 0; i < MT; ++i) {
-                        o[16 * i + g] = fmaf(acc[nt][i][e], v_back, ob[nt][e]);
-                        o[16 * i + 8 + g] = fmaf(acc[nt][i][2 + e], v_back, ob[nt][e]);
+                        o[16 * i + g] = acc[nt][i][e] + ob[nt][e];
+                        o[16 * i + 8 + g] = acc[nt][i][2 + e] + ob[nt][e];
                     }
                     if (g == 0) {
                         float *ml = near ? o + D : p.part_ml + (piece * ROWS + lr) * 2;

@@ -65,3 +65,31 @@ def test_small_weights_count_where_the_largest_stands_for_nothing(D, n, G, gap):
     assert (dv[0, 21, 0, 2:] == 0).all() and (bv[0, 21] == 0).all()
     q = torch.ones((1, n, G, D), device=DEV).half()
     check(cache.attend(0, q, scale=gap / D), *attend_reference(q, dk, dv, bv, [48 + n], gap / D))
+
+
+# ---- values of very different sizes
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("n,G", [(1, 2), (3, 4), (5, 4), (8, 4)])
+@pytest.mark.parametrize("length,at,gap", [(300, 0, 3), (300, 70, -4), (300, 64, 25), (300, 280, 3), (300, 40, 150), (7000, 3333, -2),
+                                           (7000, 3300, 20)])
+@pytest.mark.parametrize("size", [1e-1, 1e-3, 1e-4])
+def test_a_large_value_that_does_not_count_costs_the_others_nothing(D, n, G, length, at, gap, size):
+    """One token's values are the largest that the format holds. For half of the query rows its weight is exp(-40) of that of
+    the token `gap` positions on, which counts most; for the others it is nearly all."""
+    cache, order = make_cache(1, 1, D, 64, -(-length // 64), seed=2)
+    give_pages(cache, order, [length])
+    g = torch.Generator(DEV).manual_seed(at)
+    k = 0.3 * torch.randn((1, length, 1, D), generator=g, device=DEV)
+    v = size * torch.randn((1, length, 1, D), generator=g, device=DEV)
+    k[0, at + gap] = 1.5
+    k[0, at] = -6.0
+    v[0, at] = 57344.0 * (2.0 * torch.rand((1, D), generator=g, device=DEV) - 1.0)
+    k, v = k.half(), v.half()
+    cache.append(0, k, v, i32([0]))
+    (dk, _), (dv, bv) = values_of(k), values_of(v)
+    q = torch.ones((1, n, G, D), device=DEV).half()
+    q[0, :, 1::2] = -1.0                                         # these rows see the large value and little else
+    for scale in (8.0 / D, 4.0 / D):
+        got = cache.attend(0, q, scale=scale)
+        assert cache.device_status() == 0
+        check(got, *attend_reference(q, dk, dv, bv, [length], scale))
