@@ -49,7 +49,7 @@ namespace ralm {
 constexpr int kAttendMaxBatch = 4096;
 constexpr int kAttendStage = 64;         // tokens of a stage in shared memory, the largest unit of work
 constexpr float kAttendLazy = 6.f;       // a maximum may be this far (powers of two) behind before sums are rescaled
-constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8) (and 2^0.1 for log2_of_half) is below fp16's largest
+constexpr float kAttendBias = 8.f;       // exponent added to the weights: 2^(6 + 8 + 1) is below fp16's largest
 
 // Warps per CTA (one CTA per SM) and whether the query operands stay in registers, by column blocks.
 __host__ __device__ constexpr int attend_warps(int nt, int d) { return nt >= 3 ? 8 : nt == 1 && d == 64 ? 16 : 12; }
@@ -121,11 +121,12 @@ __device__ __forceinline__ void unpack4(uint32_t x, uint32_t (&y)[4]) {
 // c - 8 of the same pairs, as normal numbers: 1024 + c and 64 + c are a mask and an exponent away, the difference is exact.
 // The exponents come out of a shuffle so that the compiler holds them in ordinary registers, where mask and exponent are
 // one instruction (32 x 8 heads of 2000 to 32000 tokens: 129 us, 138 with two).
-struct Centre {
-    uint32_t e1024, e64;
-    __device__ __forceinline__ Centre() {
+struct Exponents {
+    uint32_t e1024, e64, e23;
+    __device__ __forceinline__ Exponents() {
         e1024 = __shfl_sync(0xffffffffu, 0x64006400u, threadIdx.x & 31);
         e64 = __shfl_sync(0xffffffffu, 0x54005400u, threadIdx.x & 31);
+        e23 = __shfl_sync(0xffffffffu, 0x4B000000u, threadIdx.x & 31);
     }
     __device__ __forceinline__ void unpack4(uint32_t x, uint32_t (&y)[4]) const {
         const uint32_t z = x >> 8;
@@ -134,13 +135,12 @@ struct Centre {
         y[2] = hsub2((z & 0x000F000Fu) | e1024, 0x64086408u);
         y[3] = hsub2((z & 0x00F000F0u) | e64, 0x54805480u);
     }
+    // floor(log2 x), x the fp16 number in the low half of a word; -15 for zero and subnormals. The exponent's bits, put
+    // behind those of 2^23.
+    __device__ __forceinline__ float log2_floor(uint32_t pair) const {
+        return fmaf(__uint_as_float((pair & 0x7C00u) | e23), 1.f / 1024.f, -8207.f);   // 2^23 / 1024 + 15
+    }
 };
-
-// log2 of the fp16 number in the low half of a word, within 0.09 below; up to 9 above for subnormals, -15 for zero. Its bits
-// are a number of 1024ths; put behind those of 2^23 they are one in fp32.
-__device__ __forceinline__ float log2_of_half(uint32_t pair) {
-    return fmaf(__uint_as_float(__byte_perm(pair, 0x4B000000u, 0x7610)), 1.f / 1024.f, -8207.f);   // 2^23 / 1024 + 15
-}
 
 // The largest finite absolute value of eight; infinities and NaN do not set a row's scale.
 __device__ __forceinline__ float q_top(const __half *x) {
@@ -652,7 +652,7 @@ attend_kernel(const AttendParams p) {
             if (feed.seg.b != b) feed.enter(p);
         }
     };
-    const Centre centre;
+    const Exponents exponents;
     Segment seg = mine_first;
 #pragma unroll 1
     for (int i = 0; i < STAGES; ++i) issue();
@@ -759,7 +759,8 @@ attend_kernel(const AttendParams p) {
         __syncwarp();                    // the factors are in place
         f *= p.scale * 1048576.f;        // the codes' 2^-20
 
-        // the weights are 2^(score - mb), mb a maximum of score + log2 s_v less kAttendBias
+        // the weights are 2^(score - mb), mb a maximum of score + floor(log2 s_v) less kAttendBias: that maximum's p is a power of
+        // two, and its p s_v exact in fp16
         float acc[NT][MT][4], mb[NT][2], l[NT][2], ob[NT][2];
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
@@ -813,7 +814,7 @@ attend_kernel(const AttendParams p) {
                         kb[kt][j] = (a.y - 8.f * a.x) * (f * 9.5367431640625e-7f);        // sum(q) carries no 2^-20
                         vs[kt][j] = b.x;
                         vb[kt][j] = b.y;
-                        vl[kt][j] = log2_of_half(v_pair);
+                        vl[kt][j] = exponents.log2_floor(v_pair);
                         if (masked && at + g + 8 * j >= len) vs[kt][j] = vb[kt][j] = 0.f;   // the rest of a page holds anything
                     }
                 }
@@ -933,8 +934,8 @@ attend_kernel(const AttendParams p) {
                             const uint32_t pick = half ? 0x7632 : 0x5410;
                             const uint32_t xa = __byte_perm(xv[kt][0].w[w], xv[kt][0].w[W / 2 + w], pick);
                             const uint32_t xb = __byte_perm(xv[kt][1].w[w], xv[kt][1].w[W / 2 + w], pick);
-                            centre.unpack4(xa, a);
-                            centre.unpack4(xb, b);
+                            exponents.unpack4(xa, a);
+                            exponents.unpack4(xb, b);
 #pragma unroll
                             for (int nt = 0; nt < NT; ++nt) {
                                 mma_f16(acc[nt][4 * w + 2 * half], a[0], a[1], b[0], b[1], pf[kt][nt][0], pf[kt][nt][1]);

@@ -93,3 +93,26 @@ def test_a_large_value_that_does_not_count_costs_the_others_nothing(D, n, G, len
         got = cache.attend(0, q, scale=scale)
         assert cache.device_status() == 0
         check(got, *attend_reference(q, dk, dv, bv, [length], scale))
+
+
+# ---- the weight that counts most is exact
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("size", [1.0, 0.013, 3e-5, 9000.0])
+def test_a_row_of_one_token_is_that_tokens_value(dtype, D, size):
+    """Its p is a power of two but for the rounding of the score less its reference (2^-20 where scores stay below 8), so
+    p s_v becomes a power of two times s_v in fp16, which is exact: s (c - 8) loses nothing to the weight's 11 bits. What
+    remains is 2^-19 of |v| + |b|, and the result's half unit."""
+    B, H, G = 40, 2, 4
+    cache, order = make_cache(B, H, D, 16, 1, seed=5)
+    give_pages(cache, order, [1] * B)
+    g = torch.Generator(DEV).manual_seed(5)
+    k = torch.randn((B, 1, H, D), generator=g, device=DEV).half()
+    v = (size * (torch.randn((B, 1, H, D), generator=g, device=DEV) + 0.3)).half()
+    cache.append(0, k, v, i32([0] * B))
+    want, offset = (x.repeat_interleave(G, 2) for x in values_of(v))
+    q = torch.randn((B, 1, H * G, D), generator=g, device=DEV).to(dtype)
+    got = cache.attend(0, q).double()
+    info = torch.finfo(dtype)
+    unit = torch.exp2(torch.floor(torch.log2(want.abs().clamp(min=info.tiny)))) * info.eps
+    assert ((got - want).abs() <= 0.5 * unit + 2.0 ** -19 * (want.abs() + offset.abs())).all()
