@@ -430,7 +430,8 @@ ralm_status_t ralm_pages_status(const ralm_pages_t *pages, void *stream);
 /* A key-value cache held in 4 bits over such a pool (of one page at least): page_bytes = kv_heads * page_size * (head_dim + 8),
  * head_dim 64 or 128, page_size 16, 32 or 64. A vector of one token and head is held as
  *   s = fp16((max - min) / 15), b = fp16(min + 8 s), c = clamp(rint((x - b) / s) + 8, 0, 15)
- * and stands for s (c - 8) + b. Values saturate at +-57344; a NaN counts as 0. */
+ * in 32 bits, where the divisions are products with 1 / 15 and 1 / s as rounded to 32 bits (at a tie a code
+ * can differ by one from the quotient's), and stands for s (c - 8) + b. Values saturate at +-57344; a NaN counts as 0. */
 typedef struct {
     ralm_pages_t pages;
     int32_t kv_heads, head_dim;

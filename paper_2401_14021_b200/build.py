@@ -3,7 +3,7 @@ tensor marshalling _native.so.
 
 `--debug` builds libralm_debug.so beside it with -DRALM_DEBUG_BOUNDS: every index into a global
 array that a scan kernel computes is checked against the array's extent (a violation is recorded
-in the status word as RALM_ERR_INTERNAL; nothing traps). Point RALM_LIBRARY at that file to run
+in the status word as RALM_ERR_INTERNAL; nothing traps); the generator's operators are in it as they are. Point RALM_LIBRARY at that file to run
 the tests or the benchmark on it."""
 import os
 import subprocess

@@ -11,9 +11,11 @@
 // In the second product the addends differ by far more, by the weights of a softmax: there the operand is c - 8 as a normal
 // number, two instructions shared by all query rows, and what is small beside the largest weight of a tile is not cut off.
 // The weights p s_v are rounded to fp16 (11 bits) before the second product; maxima, sums and outputs stay in
-// 32 bits. What p is relative to is, for each query row, the largest p s_v, not the largest p: so the weights that
-// count lie high in fp16's range, whatever the sizes of the values, and one large value that does not count for a
-// row costs it nothing (2^22 lie between the largest weight and the first that loses bits).
+// 32 bits. The error against 64 bits of an fp16 output is 2.7e-4 of its size with that and 2.1e-4 without (the output's
+// own rounding, which in bf16 hides the weights' altogether); the cut-off bits as a second fp16 operand would cost 12 %
+// of a decode step and 20 % of a verification. What p is relative to is, for each query row, the largest p s_v, not the
+// largest p: the weights that count lie high in fp16's range whatever the sizes of the values, and one large value that
+// does not count for a row costs it nothing (2^22 lie between the largest weight and the first that loses bits).
 //
 // A warp is a worker with its own stages in shared memory (bulk copies of 32 tokens, completion on a
 // barrier of its own): no warp waits for another, and any mix of lengths keeps all of them busy.
@@ -24,14 +26,16 @@
 //
 // Bound, with up to 8 query rows per key-value head, by the cache's bytes (136 a token and head of 128) and by
 // issue slots at almost the same rate: a tile of 16 tokens is 2176 bytes, 90 cycles of an SM's share of the memory
-// bandwidth, and about 245 instructions, 61 cycles of its four schedulers at best. Measured (32 requests of 2000 to
-// 32000 tokens, 8 heads of 128): 1 or 8 rows 122 to 130 us (4.6 to 4.9 TB/s, 0.75 of the measured copy bandwidth); 16
-// rows 205 us, 24 rows 275 us, 36 rows (two passes) 480 us, bound by the 16 matrix instructions and 50 others that 8
-// more rows cost a tile, at the issue rate that 8 to 12 warps reach. Steps: codes loaded into registers from global
-// memory 215 us; bulk copies of whole pages, one per 64 tokens 154 us; two tiles side by side 145 us; codes as
-// subnormals instead of converting them 122 us. Small calls are latency: 7.3 us for four requests of 64 tokens, of
+// bandwidth, and about 265 instructions, 66 cycles of its four schedulers at best. Measured (32 requests of 2000 to
+// 32000 tokens, 8 heads of 128): 1 row 127 us, 8 rows 133 us (4.6 and 4.5 TB/s, 0.72 and 0.69 of the measured copy
+// bandwidth); 16 rows 206 us, 24 rows 260 us, 32 rows 364 us, 36 rows (two passes) 461 us, bound by the 16 matrix
+// instructions and 50 others that 8 more rows cost a tile, at the rate that two to three warps a scheduler reach (issue
+// slots 39 % used, matrix pipe 33 %). With 64 dimensions (64 requests of 500 to 8000 tokens, 32 heads) 162 us, 0.60 of
+// the copy bandwidth: half the bytes for more than half the instructions. Steps: codes loaded into registers from
+// global memory 215 us; bulk copies of whole pages, one per 64 tokens 154 us; two tiles side by side 145 us; K's codes as
+// subnormals instead of converting them 125 us. Small calls are latency: 7.1 us for four requests of 64 tokens, of
 // which 1 is the launch, 1.4 the cut of the work, 1 the first pages, 1.7 the queries. In between the join counts: of
-// 24.9 us for 16 requests of up to 4600 tokens (8 heads, 4 rows) 3 are spent in the CTA and 5 between CTAs.
+// 24.8 us for 16 requests of up to 4600 tokens (8 heads, 4 rows) 3 are spent in the CTA and 5 between CTAs.
 #pragma once
 
 #include <cuda_bf16.h>

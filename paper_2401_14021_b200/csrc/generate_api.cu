@@ -137,8 +137,8 @@ ralm_status_t launch(void (*kernel)(P...), int64_t blocks, int threads, size_t s
 // stores overlap another's loads), and further while there are fewer CTAs than the GPU can hold; but not
 // below one vector per thread.
 // The neighbours' table has twice as many slots as neighbours, up to 16 KB: half full at most it is quicker where
-// one CTA per SM waits for it (1 row x 32000, 64 neighbours: 5.8 us, 6.4 with as many slots as neighbours), but
-// 32 KB would leave room for fewer CTAs (72 rows x 50257, 1024 neighbours: 17.2 us, 16.0 with 16 KB).
+// one CTA per SM waits for it (1 row x 32000, 64 neighbours: 6.2 us a call, 6.7 with as many slots as
+// neighbours), but 32 KB would leave room for fewer CTAs (72 rows x 50257, 1024 neighbours: 18.5 us, 16.5 with 16 KB).
 constexpr int kMixSlice = 32 * 1024;
 constexpr int kMixMaxStage = 160 * 1024;   // bytes of a slice that a CTA keeps in shared memory
 

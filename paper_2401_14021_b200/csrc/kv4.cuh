@@ -4,15 +4,16 @@
 //     [K codes: ps * D / 2][V codes: ps * D / 2][K (scale, offset): ps * 4][V (scale, offset): ps * 4]
 // bytes. A vector x of a token and head is held as
 //     s = fp16((max x - min x) / 15),  b = fp16(min x + 8 s),  c = clamp(rint((x - b) / s) + 8, 0, 15)
-// and stands for s (c - 8) + b. K codes lie token by token, dimension 2i in the low half of byte i.
+// (in 32 bits; the divisions are products with 1 / 15 and 1 / s as rounded to 32 bits) and stands for s (c - 8) + b. K codes lie token by token, dimension 2i in the low half of byte i.
 // V codes lie in blocks of 16 tokens in the order in which a warp's matrix instruction wants them:
 // token 8c + 2t + e of the block has dimension g + 8j as nibble j of the D / 16 bytes at [c][g][t][e],
 // so that lane 4g + t finds its operands in consecutive bytes and each token owns whole bytes.
 //
 // Append and read are bound by memory, 2.3 times the cache's bytes for 16-bit tensors, and close behind by
-// instructions (about five per value to quantise). Measured (16 x 509 tokens, 32 heads of 128, bf16): append 42 us and
-// read 32 us, 73 us together, 4.6 TB/s, 0.71 of the measured copy bandwidth; 210 us with a warp per token, whose V codes
-// left in pieces of two bytes. One token for each of 8 requests and back: 7 us for both launches.
+// instructions (about five per value to quantise). Measured (16 x 509 tokens, 32 heads of 128, bf16): append 43 us
+// (issue slots 73 % used) and read 29 us, 72 to 74 us together, 4.6 TB/s, 0.71 of the measured copy bandwidth; 210 us with
+// a warp per token, whose V codes left in pieces of two bytes. One token for each of 8 requests and back: 6.3 us for both
+// launches.
 #pragma once
 
 #include <cuda_bf16.h>

@@ -6,11 +6,12 @@
 // Bound by memory: a logit is read once and a probability written once (6 bytes an entry in 16 bits). One pass
 // over global memory therefore, the slice of a row waiting in shared memory between maximum, sum and output,
 // and a cluster per row, so that a row of 128000 entries is spread over eight SMs' shared memory. Measured (512
-// rows x 128000, bf16, 64 neighbours): 70 us, 5.6 TB/s, 0.87 of the measured copy bandwidth; without neighbours 65 us.
+// rows x 128000, bf16, 64 neighbours): 72 to 76 us, 5.2 to 5.5 TB/s, 0.80 to 0.85 of the measured copy bandwidth; without
+// neighbours 66 us.
 // Stores had to be 16 bytes per thread and aligned whatever the input's alignment (333 -> 127 us with the slice
 // staged), and the exchange between CTAs one store per warp instead of block and cluster barriers (127 -> 76 us).
-// A single row of 32000 takes 4.7 us, 6.1 us with neighbours (ids, then the values they point at: two more
-// round trips to memory).
+// A single row of 32000 takes 3.8 us in a CUDA graph, 4.9 us with neighbours (ids, then the values they point at: two more
+// round trips to memory); called one by one 6.2 us, what the host needs for a launch.
 #pragma once
 
 #include <cooperative_groups.h>
@@ -27,6 +28,7 @@ namespace cg = cooperative_groups;
 
 constexpr float kLog2e = 1.4426950408889634f;
 
+// 2^x within 2 units of 2^-23 of it; below 2^-126 it is 0.
 __device__ __forceinline__ float exp2_approx(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));

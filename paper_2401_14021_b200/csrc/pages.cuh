@@ -7,7 +7,9 @@
 //
 // The bookkeeping is latency (a few dependent round trips in one CTA: 5 to 10 us), the copies are bandwidth (two
 // bytes of traffic per byte moved). Measured: 256 of 1024 pages of 70 KB in 32 layers moved in 196 us, 5.8 TB/s, 0.90
-// of the measured copy bandwidth; fork, copy on write for 16 pairs in 24 layers and roll back in 23 us.
+// of the measured copy bandwidth; fork, copy on write for 16 pairs in 24 layers and roll back in 23 us. Admission is the
+// serial part: one thread writes a row's pages one after another (64 prompts of 2000 to 32000 tokens in and out again:
+// 88 us with 64 tokens a page, 584 us with 16).
 #pragma once
 
 #include <cuda_runtime.h>

@@ -6,9 +6,9 @@
 // have no order, so any split over lanes, warps and CTAs gives the same token.
 //
 // Bound by memory: only the row of the first rejection is read (p and q, 8 bytes an entry), once, plus the run of
-// it that holds the drawn token. Measured (256 requests, 8 drafts, 128000 entries): 50 us, 5.3 TB/s, 0.82 of the
-// measured copy bandwidth; 64 requests of 50257 entries with certain drafts 9 us; one request 6 us, three dependent
-// round trips to memory. Rows are read 4 bytes per lane, coalesced, eight loads in flight, because p's and q's rows
+// it that holds the drawn token. Measured (256 requests, 8 drafts, 128000 entries): 52 us, 5.1 TB/s, 0.79 of the
+// measured copy bandwidth; 64 requests of 50257 entries with certain drafts 10.3 us (7.8 us in a CUDA graph); one request
+// 6.2 us (5.3), three dependent round trips to memory. Rows are read 4 bytes per lane, coalesced, eight loads in flight, because p's and q's rows
 // of an odd vocabulary never share an alignment; the sums in two 32-bit words (nine plain instructions a term)
 // instead of 64-bit shifts took 256 requests from 164 to 49 us.
 #pragma once

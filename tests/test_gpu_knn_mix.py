@@ -1,8 +1,10 @@
 """The KNN-LM mixture against its definition in 64 bits.
 
 Tolerance, set from the arithmetic: an exponent x log2(e) / T - r is rounded once at its own size (below 200
-wherever the result is above 1e-60), 200 * 2^-24 * ln 2 = 8e-6 relative; the approximate 2^x adds 2^-22, the sums and
-the normalisation a few 2^-24. Neighbours: weights at 2^-22, their sum in 54-bit fixed point. So 2e-5 relative."""
+wherever the result is above 1e-60), 200 * 2^-24 * ln 2 = 8e-6 relative, and its factor log2(e) / T, the same for the whole
+row, is within 2^-23 (below 2^22 powers of two; the rest is in test_gpu_knn_mix_extremes.py); the approximate 2^x adds
+2^-22, the sums and the normalisation a few 2^-24. Neighbours: weights at 2^-22, their sum in 42-bit fixed point relative
+to the token's largest. So 2e-5 relative."""
 import math
 
 import pytest
