@@ -49,6 +49,10 @@ struct Runs {
         while (i < 3 && a.n[i] == 1) ++i;
         while (j < 3 && b.n[j] == 1) ++j;
         if (i == 3 && j == 3) return true;
+        if (i < 3 && j < 3 && a.step[i] == b.step[j]) {              // side by side in every part of one buffer
+            const int64_t s = a.step[i], behind = ((pb - pa) % s + s) % s;
+            if (a.extent[i + 1] <= behind && behind + b.extent[j + 1] <= s) return false;
+        }
         if (i == 3 || (j < 3 && eb > ea)) return meet(b, j, pb, a, i, pa);
         // those parts of a that reach into b's range
         const int64_t s = a.step[i], part = a.extent[i + 1];

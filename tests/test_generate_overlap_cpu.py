@@ -71,16 +71,20 @@ def test_verify_tokens(lib):
         assert call(**kw) == CUDA, kw
 
 
+class AttendArgs(ctypes.Structure):
+    _fields_ = [("q", p), ("out", p)] + [(x, i64) for x in ("qb", "qn", "qh", "ob", "on", "oh")] + [
+        (x, i32) for x in ("batch", "n", "q_heads", "dtype")] + [("scale", f32), ("rows", p), ("q_len", p), ("workspace", p), ("size", i64)]
+
+
+def cache():
+    from paper_2401_14021_b200.generate import _Kv, _Pages
+    return _Kv(pages=_Pages(pool=256, layers=1, layer_stride=1152 * 16, page_bytes=1152, pages=16, rows=64, max_pages=8, page_size=16, table=256,
+                            lengths=256, refs=256, status=256, workspace=256), kv_heads=1, head_dim=64)
+
+
 def test_attention(lib):
     """Random layouts in one buffer against sets of bytes."""
-    from paper_2401_14021_b200.generate import _Kv, _Pages
-    kv = _Kv(pages=_Pages(pool=256, layers=1, layer_stride=1152 * 16, page_bytes=1152, pages=16, rows=64, max_pages=8, page_size=16, table=256,
-                          lengths=256, refs=256, status=256, workspace=256), kv_heads=1, head_dim=64)
-
-    class Attend(ctypes.Structure):
-        _fields_ = [("q", p), ("out", p)] + [(x, i64) for x in ("qb", "qn", "qh", "ob", "on", "oh")] + [
-            (x, i32) for x in ("batch", "n", "q_heads", "dtype")] + [("scale", f32), ("rows", p), ("q_len", p), ("workspace", p), ("size", i64)]
-
+    kv, Attend = cache(), AttendArgs
     rng = random.Random(1)
     seen = {OK: 0, INVALID: 0, CUDA: 0}
     for _ in range(3000):
@@ -104,3 +108,22 @@ def test_attention(lib):
         assert got == (INVALID if sets[0] & sets[1] else CUDA), (n, where)
         seen[got] += 1
     assert seen[INVALID] > 300 and seen[CUDA] > 300, seen
+
+
+def test_columns_of_one_buffer_are_told_apart_at_once(lib):
+    """Queries, outputs and others in turn for each token, as a fused projection leaves them: however many tokens, the
+    answer takes no look at each."""
+    import time
+
+    kv, Attend = cache(), AttendArgs
+    took = []
+    for n in (1000, 200000):
+        row = 3 * 4 * 64
+        for shift, want in ((4 * 64, CUDA), (4 * 64 - 8, INVALID), (2 * 4 * 64, CUDA), (row - 64, INVALID), (-4 * 64, CUDA), (-4 * 64 + 8, INVALID)):
+            q = BASE << 8
+            a = Attend(q, q + 2 * shift, n * row, row, 64, n * row, row, 64, 1, n, 4, 0, 1.0, None, None, 256, 1 << 60)
+            begin = time.perf_counter()
+            assert lib.ralm_kv_attend(ctypes.addressof(kv), 0, ctypes.addressof(a), None) == want, (n, shift)
+            if want == CUDA:
+                took.append(time.perf_counter() - begin)
+    assert sorted(took)[len(took) // 2] < 1e-3
