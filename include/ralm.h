@@ -455,7 +455,7 @@ typedef struct {
 ralm_status_t ralm_kv_append(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream);
 
 /* The values that positions starts .. starts + n - 1 stand for; zeros at positions outside the row or
- * beyond `count`. */
+ * beyond `count`. K and V must not overlap (INVALID_ARG). */
 ralm_status_t ralm_kv_read(const ralm_kv_t *cache, int32_t layer, const ralm_kv_tokens_t *tokens, void *stream);
 
 /* Attention of the newest tokens over the cache: query i of an entry with m = q_len queries (n where

@@ -233,6 +233,10 @@ ralm_status_t kv_tokens(bool append, const ralm_kv_t *c, int32_t layer, const ra
     if (c->head_dim != 64 && c->head_dim != 128) return RALM_ERR_UNSUPPORTED;
     if (t->batch == 0 || t->n == 0) return RALM_OK;
     if (!t->k || !t->v || !t->starts) return RALM_ERR_INVALID_ARG;
+    if (!append &&                                                   // K and V of a read are both written
+        Runs(t->k, 2LL * c->head_dim, {{t->batch, 2 * t->k_stride_b}, {t->n, 2 * t->k_stride_n}, {c->kv_heads, 2 * t->k_stride_h}})
+            .overlaps(Runs(t->v, 2LL * c->head_dim, {{t->batch, 2 * t->v_stride_b}, {t->n, 2 * t->v_stride_n}, {c->kv_heads, 2 * t->v_stride_h}})))
+        return RALM_ERR_INVALID_ARG;
     const int sms = sm_count();
     if (sms == 0) return RALM_ERR_CUDA;
     const KvParams k = kv_params(*c, layer, t->rows, t->batch);

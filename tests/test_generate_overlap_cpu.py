@@ -127,3 +127,15 @@ def test_columns_of_one_buffer_are_told_apart_at_once(lib):
             if want == CUDA:
                 took.append(time.perf_counter() - begin)
     assert sorted(took)[len(took) // 2] < 1e-3
+
+
+def test_read(lib):
+    class Tokens(ctypes.Structure):
+        _fields_ = [("k", p), ("v", p), ("strides", i64 * 6), ("batch", i32), ("n", i32), ("dtype", i32), ("rows", p), ("starts", p), ("count", p)]
+
+    kv = cache()
+    for call, k, v, want in ((lib.ralm_kv_read, BASE, BASE, INVALID), (lib.ralm_kv_read, BASE, BASE + 120, INVALID),
+                             (lib.ralm_kv_read, BASE, BASE + 128, CUDA), (lib.ralm_kv_append, BASE, BASE, CUDA)):
+        t = Tokens(k, v, (i64 * 6)(1280, 128, 64, 1280, 128, 64), 3, 10, 0, None, 256, None)
+        call.argtypes = [p, i32, p, p]
+        assert call(ctypes.addressof(kv), 0, ctypes.addressof(t), None) == want
