@@ -281,8 +281,8 @@ mix_kernel(const MixParams p) {
         for (int j = 0; j < kMixNeighbours; ++j) {
             own[j] = in_slot[j] = -1;
             if (token[j] < 0) continue;
-            // the weight from here on: differences are scaled, so that no finite score is too large to count
-            score[j] = exp2_approx((score[j] - best) * p.score_scale);
+            // the weight from here on: differences are scaled, and halves subtracted, so that no finite score is too large
+            score[j] = exp2_approx(2.f * (fmaf(score[j], 0.5f, -0.5f * best) * p.score_scale));
             sum += score[j];
             const int pos = token[j] - base;
             if (pos < 0 || pos >= p.slice) continue;

@@ -116,6 +116,20 @@ def test_scores_of_any_size():
             check(got, reference(logits, ids, scores, values, 0.6, 1.0, tau, sign))
 
 
+def test_scores_whose_difference_is_not_finite():
+    ralm = _ralm()
+    R, V, k = 3, 97, 24
+    g = torch.Generator(DEV).manual_seed(8)
+    logits = torch.randn((R, V), generator=g, device=DEV)
+    ids, _, values = neighbours(R, V, k, 9)
+    scores = 3.3e38 * (2.0 * torch.rand((R, k), generator=g, device=DEV) - 1.0)
+    scores[:, 0], scores[:, 1] = 3.4e38, -3.4e38
+    for metric, sign in ((ralm.IP, 1), (ralm.L2, -1)):
+        for tau in (3e38, 1e38, 1e37):
+            got = ralm.knn_mix(logits, ids, scores, values, 0.6, knn_temperature=tau, metric=metric)
+            check(got, reference(logits, ids, scores, values, 0.6, 1.0, tau, sign))
+
+
 def test_temperatures_whose_inverse_is_not_finite_are_refused():
     ralm = _ralm()
     logits, (ids, scores, values) = torch.randn((2, 50), device=DEV), neighbours(2, 50, 3, 7)
