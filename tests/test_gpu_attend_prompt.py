@@ -8,6 +8,11 @@ from test_gpu_kv_cache import DEV, attend_reference, check, filled, i32
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def same_inputs_every_time():
+    torch.manual_seed(0)
+
+
 @pytest.mark.parametrize("D,ps", [(64, 16), (128, 64)])
 @pytest.mark.parametrize("n,H,G,lengths", [(10, 2, 1, [10]), (33, 1, 1, [33, 40]), (33, 2, 3, [33, 5, 300]), (128, 1, 4, [128, 161]),
                                            (130, 2, 1, [130, 131, 700]), (509, 1, 4, [509, 1000])])

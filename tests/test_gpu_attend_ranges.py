@@ -7,6 +7,11 @@ from test_gpu_kv_cache import DEV, attend_reference, check, give_pages, i32, mak
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def same_inputs_every_time():
+    torch.manual_seed(0)
+
+
 def values_of(x):
     held, _, offset = stands_for(x)
     return torch.from_numpy(held).to(DEV), torch.from_numpy(offset).to(DEV)

@@ -7,6 +7,11 @@ from test_gpu_kv_cache import DEV, give_pages, i32, make_cache
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def same_inputs_every_time():
+    torch.manual_seed(0)
+
+
 # ---- entries without tokens, positions outside a row
 @pytest.mark.parametrize("D", [64, 128])
 def test_an_entry_without_tokens_is_no_error(D):

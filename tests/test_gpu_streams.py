@@ -7,6 +7,11 @@ from test_gpu_kv_cache import DEV, attend_reference, check, filled, i32
 pytestmark = pytest.mark.gpu
 
 
+@pytest.fixture(autouse=True)
+def same_inputs_every_time():
+    torch.manual_seed(0)
+
+
 def busy(milliseconds=60):
     """Keeps the current stream busy; the event that is returned comes after that."""
     torch.cuda._sleep(int(milliseconds * 1.9e6))
