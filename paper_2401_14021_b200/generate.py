@@ -139,7 +139,7 @@ class Pages:
 
 class KVCache(Pages):
     """A key-value cache held in 4 bits (ralm_kv_t) over a page pool of kv_heads * page_size *
-    (head_dim + 8) bytes per page; head_dim 64 or 128, page_size 16, 32 or 64. Attention's workspace (25 to 50 MB) is
+    (head_dim + 8) bytes per page; head_dim 64 or 128, page_size 16, 32 or 64. Attention's workspace (23 MB for head_dim 64, 46 MB for 128) is
     made and cleared here, on the current stream; a call on another one comes after that, as with any tensor."""
 
     def __init__(self, pool: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, refs: torch.Tensor, *,

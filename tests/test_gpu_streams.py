@@ -93,3 +93,43 @@ def test_results_of_a_read_on_another_stream(given):
     for x, y in zip(got, want):
         assert torch.equal(x, y)
     assert got[0].dtype is torch.float16 and cache.device_status() == 0
+
+
+def test_pages_and_tokens_on_another_stream():
+    """Every call of the pages and the cache, in turn, on a stream that does not wait for the busy current one."""
+    import paper_2401_14021_b200 as ralm
+    x = torch.randn((3, 40, 2, 64), device=DEV).half()
+    zero, lengths, grown = i32([0, 0, 0]), i32([40, 17, 0]), i32([40, 17, 43])
+    new, starts, row = torch.randn((1, 3, 2, 64), device=DEV).half(), i32([40]), i32([2])
+    src, dst = i32([0]), i32([2])
+    out = torch.empty((3, 1, 4, 64), dtype=torch.float16, device=DEV)
+    q = torch.randn((3, 1, 4, 64), device=DEV).half()
+    k, v = (torch.empty((1, 43, 2, 64), dtype=torch.float16, device=DEV) for _ in range(2))
+
+    def make():
+        return ralm.KVCache.allocate(1, 2, 64, pages=12, rows=3, max_pages=4, page_size=16, device=DEV)
+
+    def use(cache, stream):
+        cache.resize(lengths, stream=stream)
+        cache.append(0, x, x, zero, count=lengths, stream=stream)
+        cache.fork(src, dst, stream=stream)
+        cache.resize(grown, stream=stream)
+        cache.append(0, new, new, starts, rows=row, stream=stream)
+        cache.compact(stream=stream)
+        cache.read(0, zero[:1], 43, rows=row, k=k, v=v, stream=stream)
+        cache.attend(0, q, out=out, stream=stream)
+
+    first, second = make(), make()
+    use(first, None)
+    want = [t.clone() for t in (first.table, first.lengths, first.refs, k, v, out)]
+    for t in (k, v, out):
+        t.zero_()
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    done = busy()
+    use(second, side)
+    assert second.device_status(stream=side) == 0
+    assert not done.query()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip((second.table, second.lengths, second.refs, k, v, out), want))
+    assert first.device_status() == 0
